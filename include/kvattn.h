@@ -293,6 +293,77 @@ typedef struct {
 kv_status_t attn_mixed(kv_pool_t* pool, int n_q_heads, float scale, const attn_extend_args_t* ext,
                        const attn_decode_args_t* dec, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- around attention in a step -------------------------------------------------------------
+ * (The paper has no counterpart of these calls: its engine does this work.  They take a step from its sequences' lengths and the
+ * projected rows of its tokens to stored pages, and a query to the pages worth attending over.)
+ * A slot is a place for a token: 16 * page + place in the page.  A slot map has a slot for every row of a step, or a negative
+ * number for a row of padding; the rows that go into one page follow one another in increasing slots, as they do when every
+ * sequence's rows are in order.  Pools of more than 2^27 pages: KV_ERR_UNSUPPORTED. */
+
+/* Block tables, positions and slots of a step, from lengths that are on the device.  Sequence i holds ctx_lens[i] tokens and stores
+ * new_lens[i] more (0 or more; ctx_lens, new_lens [dev][batch]).  Each page that this opens is taken from new_pages [dev]
+ * [n_new_pages] (ids from kv_alloc) in the order of the sequences, beginning at entry *cursor [dev] (NULL: 0), and written to the
+ * sequence's row of block_tables [dev][batch][max_pages]; other entries stay.  Written besides: cu_new [dev][batch+1], the sequences'
+ * first rows; for row r of sequence i, positions[r] = ctx_lens[i] + r - cu_new[i] (positions NULL: not wanted) and slots[r]
+ * (both [dev][total_new]); rows behind the last sequence get position 0 and slot -1, so total_new may be an upper bound;
+ * next_lens[i] = ctx_lens[i] + new_lens[i] [dev][batch] (NULL: not wanted), *next_cursor = *cursor + pages taken (NULL: not wanted).
+ * next_lens may be ctx_lens and next_cursor may be cursor (a step that is captured once and replayed); no other overlap.
+ * A sequence gets nothing - no page, slots -1, position 0, next_lens = ctx_lens - and KV_ERR_BOUNDS is recorded, if a length is
+ * negative, its tokens go beyond max_pages pages or its rows beyond total_new, or new_pages has run out (then no later sequence gets
+ * a page either).  A page id outside the pool gives its rows slot -1 and records KV_ERR_BOUNDS.  KV_ERR_UNSUPPORTED: total_new or
+ * n_new_pages above 2^30. */
+kv_status_t kv_step_tables(kv_pool_t* pool, const int* ctx_lens, const int* new_lens, int batch, const int* new_pages, int n_new_pages,
+                           int* block_tables, int max_pages, int total_new, int* cu_new, int* positions, int* slots, int* next_lens,
+                           const int* cursor, int* next_cursor, void* stream);
+
+/* Rotary positions and the append in one pass.  q [dev] bf16 [total_new][n_q_heads][head_dim] is rotated into q_out, k_new [dev] bf16
+ * [total_new][n_kv_heads][head_dim] into the pages, v_new goes into the pages as it is; *_stride: elements from token to token (so the
+ * three may be parts of one projection's rows).  Pair j < rot_dim / 2 of a head's dims turns by positions[axis][row] * inv_freq[j]:
+ *     x1' = x1 cos - x2 sin,  x2' = x2 cos + x1 sin,   (x1, x2) = dims (j, j + rot_dim/2), or (2j, 2j+1) if neighbours != 0,
+ * axis = freq_axis[j] (NULL with n_axes 1: axis 0): one axis for text, several (time, height, width) for images and film.  Dims from
+ * rot_dim on pass.  Angles are formed in 64 bits, rows rotated in 32 and rounded once.  positions [dev][n_axes][total_new], inv_freq
+ * [dev] fp32 [rot_dim/2], freq_axis [dev][rot_dim/2].
+ * Row r goes to slots[r] [dev][total_new]; the last row of a page clears the slots behind it, as kv_append does.  A row with a
+ * negative slot is padding: nothing of it is written, q_out neither.  q (with q_out) may be NULL; k_new and v_new may both be NULL,
+ * and then slots too.  q_out may be q (with the same stride); no other overlap.
+ * KV_ERR_UNSUPPORTED: rot_dim not a multiple of 16 in 16 .. head_dim.  KV_ERR_INVALID: a pointer to rows not 16-byte aligned, or, with
+ * more than one row, a stride below a token's elements or not a multiple of 8.  A slot outside the pool (its row is skipped) or an axis outside 0 .. n_axes - 1 (axis 0 is
+ * taken) is recorded as KV_ERR_BOUNDS. */
+kv_status_t kv_append_rotary(kv_pool_t* pool, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new,
+                             int64_t v_stride, int n_q_heads, const int* slots, const int* positions, int n_axes, const float* inv_freq,
+                             const int* freq_axis, int rot_dim, int neighbours, int total_new, void* q_out, int64_t q_out_stride,
+                             void* stream);
+
+/* Bounds of the keys of every page that rows have been stored in: bounds [dev] bf16 [num_pages][n_kv_heads][2][head_dim],
+ * kv_page_bounds_bytes() bytes, 16-byte aligned, the caller's; [..][0][d] is the smallest and [..][1][d] the largest k_d among the page's
+ * tokens (0 .. the slot of its last row in this call).  slots [dev][total_new] as the rows were stored with; the pages hold these keys
+ * already.  Bounds of other pages stay.  A key element that is not a number makes both bounds of its dim not a number. */
+size_t kv_page_bounds_bytes(const kv_pool_t* pool);
+kv_status_t kv_page_bounds(kv_pool_t* pool, const int* slots, int total_new, void* bounds, void* stream);
+
+/* The pages worth attending over.  For every sequence and KV head, of the ceil(ctx_lens[i]/16) pages of its context: the n_first first
+ * and n_last last ones, and those others with the largest
+ *     score(page) = max over the query heads of the group of sum_d (q_d >= 0 ? q_d * hi_d : q_d * lo_d),
+ * which no key of the page exceeds, n_select in all (all pages, if there are no more).  Equal scores: the lower page first; a score that
+ * is not a number ranks above all.  The choice is that of exact scores (of sums in 64 bits).
+ * q [dev] bf16 [batch][n_q_heads][head_dim]; bounds as kv_page_bounds writes them, for all those pages; pages [dev][batch][n_kv_heads]
+ * [n_select] receives the pages as blocks of the sequence (indices into its block-table row), ascending, then -1; counts [dev][batch]
+ * [n_kv_heads] how many.  ctx_lens[i] <= 0: none.  max_ctx_len: host upper bound; a longer sequence is recorded as KV_ERR_BOUNDS and its
+ * rows are left unwritten, and so is a block-table entry outside the pool (its row's pages are then not to be trusted).
+ * KV_ERR_INVALID: n_first + n_last > n_select.  KV_ERR_UNSUPPORTED: max_ctx_len above 24576 pages. */
+kv_status_t attn_select_pages(kv_pool_t* pool, const void* q, int n_q_heads, const void* bounds, const int* block_tables, int max_pages,
+                              const int* ctx_lens, int batch, int max_ctx_len, int n_select, int n_first, int n_last, int* pages,
+                              int* counts, void* stream);
+
+/* Decode over listed pages: attn_decode whose query heads of KV head h attend over the tokens of blocks pages[i][h][0 .. counts[i][h]) of
+ * sequence i only (pages [dev][batch][n_kv_heads][width], counts [dev][batch][n_kv_heads], as attn_select_pages writes them; any order,
+ * each block once).  counts 0 or ctx_lens[i] <= 0 writes O = 0, LSE = -inf.  Entries of the list past the count are not read.
+ * A listed block that the sequence has not got is passed over, and a count outside 0 .. width leaves the rows of its KV head unwritten;
+ * both are recorded as KV_ERR_BOUNDS.  No workspace.  Other arguments and errors as for attn_decode. */
+kv_status_t attn_decode_selected(kv_pool_t* pool, const void* q, int n_q_heads, const int* block_tables, int max_pages, const int* ctx_lens,
+                                 int batch, int max_ctx_len, const int* pages, const int* counts, int width, float scale, void* out,
+                                 float* lse, void* stream);
+
 /* ---- checks ------------------------------------------------------------------------------- */
 /* Validates on the device that every block-table entry a batch would read (blocks 0..ceil(len/16)-1
  * of each row) is a page of this pool and that 0 <= lens[i] <= 16*max_pages; synchronises; returns

@@ -9,7 +9,7 @@ namespace kvattn {
 size_t decode_workspace_bytes(int n_q_heads, int head_dim, int batch, int max_ctx_len);
 kv_status_t launch_decode(kv_pool_t* p, const void* q, int n_q_heads, const int* block_tables, int max_pages,
                           const int* ctx_lens, int batch, int max_ctx_len, float scale, void* out, float* lse,
-                          cudaStream_t st, bool beside = false);
+                          cudaStream_t st, bool beside = false, const PageLists* lists = nullptr);
 kv_status_t launch_extend_small(kv_pool_t* p, const void* q, int n_q_heads, const int* cu_q, const int* block_tables,
                                 int max_pages, const int* prefix_lens, const int* extend_lens, int batch,
                                 int max_extend_len, int max_total_len, float scale, void* out, float* lse,
@@ -422,6 +422,22 @@ kv_status_t attn_decode(kv_pool_t* p, const void* q, int n_q_heads, const int* b
                         void* workspace, size_t workspace_bytes, void* stream) {
   return decode_impl(p, q, n_q_heads, block_tables, max_pages, ctx_lens, batch, max_ctx_len, scale, out, lse, workspace,
                      workspace_bytes, stream, false);
+}
+
+kv_status_t attn_decode_selected(kv_pool_t* p, const void* q, int n_q_heads, const int* block_tables, int max_pages, const int* ctx_lens,
+                                 int batch, int max_ctx_len, const int* pages, const int* counts, int width, float scale, void* out,
+                                 float* lse, void* stream) {
+  if (p == nullptr || batch < 0 || max_pages < 0 || max_ctx_len < 0 || width < 1) return KV_ERR_INVALID;
+  if (!heads_supported(p, n_q_heads)) return KV_ERR_UNSUPPORTED;
+  if (batch == 0) return KV_OK;
+  if (q == nullptr || block_tables == nullptr || ctx_lens == nullptr || pages == nullptr || counts == nullptr || out == nullptr || lse == nullptr)
+    return KV_ERR_INVALID;
+  if ((((uintptr_t)q) | ((uintptr_t)out)) & 15) return KV_ERR_INVALID;
+  if (max_ctx_len > (int64_t)max_pages * kPageSize) return KV_ERR_INVALID;
+  if (!on_pool_device(p)) return KV_ERR_INVALID;
+  const PageLists lists{pages, counts, width};
+  return launch_decode(p, q, n_q_heads, block_tables, max_pages, ctx_lens, batch, max_ctx_len == 0 ? 1 : max_ctx_len, scale, out, lse,
+                       (cudaStream_t)stream, false, &lists);
 }
 
 kv_status_t attn_mixed(kv_pool_t* p, int n_q_heads, float scale, const attn_extend_args_t* ext,

@@ -34,6 +34,7 @@ struct DecodeArgs {
   int per_cta;       // pairs a CTA takes, kWarps / per_cta warps each (1 where splits > 1)
   int len_bound;     // host-side bound on ctx_lens, up to a multiple of kDecodeChunkTokens (a longer sequence is reported and skipped)
   int wait_mode;     // kWaitFirst / kWaitLast
+  PageLists lists;   // the pages to attend over (SEL)
   float scale_log2;  // scale * log2(e)
   __nv_bfloat16* out;
   float* lse;
@@ -70,9 +71,10 @@ constexpr int decode_smem_bytes() {
   return (RING ? DecodeSmem<D>::kRing : DecodeSmem<D>::kPart) + DecodeSmem<D>::kIn + (int)sizeof(DecodeShared);
 }
 
+// SEL: the pages of a pair are those of its list, not all of the sequence's.
 // MULTI: several pairs per CTA (a.per_cta > 1).  An instantiation of its own: with the pair as a run-time value everywhere the
 // others lost 0.3 us (13 sequences of 200-3000 tokens, 64 dims, 13.2 -> 13.5; one of 517 4.25 -> 4.5).
-template <int D, bool RING, bool MULTI>
+template <int D, bool RING, bool MULTI, bool SEL>
 __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeArgs a) {
   using SM = DecodeSmem<D>;
   constexpr int NJ = D / 32, NU = D / 64;
@@ -105,10 +107,12 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
   if (a.wait_mode == kWaitFirst) ptx::dependency_wait();
 
   const int L = ptx::ld_plain(a.ctx_lens + seq);
-  const bool fits = L <= a.max_pages * kPageSize && L <= a.len_bound;
+  const int in_list = SEL ? ptx::ld_plain(a.lists.counts + unit) : 0;
+  const bool fits = L <= a.max_pages * kPageSize && L <= a.len_bound && (!SEL || (unsigned)in_list <= (unsigned)a.lists.width);
   if (!fits && rank == 0 && lane == 0) report(a.pool.status, KV_ERR_BOUNDS);  // left unwritten
   if (MULTI && lane == 0 && warp == mine * team) sh.fits[mine] = fits;
-  const int n_pages = fits && L > 0 && !idle ? (L + kPageSize - 1) / kPageSize : 0;
+  const int blocks = fits && L > 0 && !idle ? (L + kPageSize - 1) / kPageSize : 0;  // of the sequence
+  const int n_pages = !SEL ? blocks : blocks > 0 ? in_list : 0;
   const int runs = team * splits;
   const int run = rank * team + warp - mine * team;
   const int p_begin = (int)((int64_t)n_pages * run / runs), p_end = (int)((int64_t)n_pages * (run + 1) / runs);
@@ -131,10 +135,22 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
     const char* vbase = reinterpret_cast<const char*>(a.pool.v) + (size_t)kvh * blk;
     const size_t page_stride = (size_t)Hkv * blk;
     const int* bt_row = a.block_tables + (int64_t)seq * a.max_pages;
-    auto table_entry = [&](int p) {
+    const int* list = SEL ? a.lists.pages + (int64_t)unit * a.lists.width : nullptr;
+    // p: place in the pair's run of pages; block: which of the sequence's it is (SEL: as listed; none, all of whose keys are
+    // hidden, if the sequence has no such block)
+    auto table_entry = [&](int p, int& block) {
       int pg = 0;
+      block = p;
       if (p < p_end) {
-        pg = ptx::ld_plain(bt_row + p);
+        if constexpr (SEL) {
+          block = ptx::ld_plain(list + p);
+          if ((unsigned)block >= (unsigned)blocks) {
+            report(a.pool.status, KV_ERR_BOUNDS);
+            block = blocks;
+            return pg;
+          }
+        }
+        pg = ptx::ld_plain(bt_row + block);
         if ((unsigned)pg >= (unsigned)a.pool.num_pages) {
           report(a.pool.status, KV_ERR_BOUNDS);
           pg = 0;  // stay inside the pool; the result of this row is flagged, not trusted
@@ -143,7 +159,8 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
       return pg;
     };
     // Block-table entries: 32 per batch, the next batch asked for while this one is walked.
-    int cur = table_entry(p_begin + lane), nxt = table_entry(p_begin + 32 + lane);
+    int cur_block, nxt_block;
+    int cur = table_entry(p_begin + lane, cur_block), nxt = table_entry(p_begin + 32 + lane, nxt_block);
     int base = p_begin;  // page of cur's lane 0
     auto page_id = [&](int p) {  // p in [base, base + 64); the whole warp calls
       const int i = p - base;
@@ -152,10 +169,12 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
     auto advance = [&](int p) {
       if (p - base >= 32) {
         cur = nxt;
+        cur_block = nxt_block;
         base += 32;
-        nxt = table_entry(base + 32 + lane);
+        nxt = table_entry(base + 32 + lane, nxt_block);
       }
     };
+    auto first_token = [&](int p) { return (SEL ? __shfl_sync(0xffffffffu, cur_block, (p - base) & 31) : p) * kPageSize; };  // p in [base, base + 32)
     if constexpr (RING) {
       const uint32_t slots = ptx::smem_u32(smem_raw) + warp * (kStages * SM::kSlot);
       const uint32_t bars = ptx::smem_u32(&sh.bars[warp * kStages]);
@@ -186,7 +205,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
         __syncwarp();
         ptx::fence_proxy_async_smem();
         if (p + kStages < p_end) issue(p + kStages);
-        page_step<D>(st, pr, qf, p * kPageSize, limit0, limit1, L, a.scale_log2, r, c);
+        page_step<D>(st, pr, qf, first_token(p), limit0, limit1, L, a.scale_log2, r, c);
       }
       if (!ok && lane == 0) {  // a wait gave up: flag it and let the copies that were asked for land (bounded)
         report(a.pool.status, KV_ERR_TIMEOUT);
@@ -200,7 +219,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
         const int pg = page_id(p);
         PageRegs<D> pr;
         load_page<D>(pr, kbase + (size_t)pg * page_stride, vbase + (size_t)pg * page_stride, r, c);
-        page_step<D>(st, pr, qf, p * kPageSize, limit0, limit1, L, a.scale_log2, r, c);
+        page_step<D>(st, pr, qf, first_token(p), limit0, limit1, L, a.scale_log2, r, c);
       }
     }
   }
@@ -305,13 +324,13 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
 std::atomic<int> g_decode_impl{0};  // 0: by the pages per warp, 1: pages stream through registers, 2: pages go through a shared-memory ring
 
 // Prepares a variant of the kernel for the current device; asking for its attributes loads its code.
-template <int D, bool RING, bool MULTI>
+template <int D, bool RING, bool MULTI, bool SEL>
 static kv_status_t prepare_variant() {
   cudaFuncAttributes at;
-  KV_CUDA_OK(cudaFuncGetAttributes(&at, attn_decode_kernel<D, RING, MULTI>));
-  KV_CUDA_OK(cudaFuncSetAttribute(attn_decode_kernel<D, RING, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  KV_CUDA_OK(cudaFuncGetAttributes(&at, attn_decode_kernel<D, RING, MULTI, SEL>));
+  KV_CUDA_OK(cudaFuncSetAttribute(attn_decode_kernel<D, RING, MULTI, SEL>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                   decode_smem_bytes<D, RING>()));
-  KV_CUDA_OK(cudaFuncSetAttribute(attn_decode_kernel<D, RING, MULTI>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+  KV_CUDA_OK(cudaFuncSetAttribute(attn_decode_kernel<D, RING, MULTI, SEL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   return KV_OK;
 }
 
@@ -321,9 +340,13 @@ static kv_status_t decode_setup(int device) {
   static std::atomic<bool> configured[kMaxDevices];
   if (device < 0 || device >= kMaxDevices) return KV_ERR_INVALID;
   if (!configured[device].load(std::memory_order_acquire)) {
-    kv_status_t (*const all[])() = {prepare_variant<128, true, false>, prepare_variant<128, false, false>, prepare_variant<128, true, true>,
-                                    prepare_variant<128, false, true>, prepare_variant<64, true, false>,   prepare_variant<64, false, false>,
-                                    prepare_variant<64, true, true>,   prepare_variant<64, false, true>};
+    kv_status_t (*const all[])() = {
+        prepare_variant<128, true, false, false>, prepare_variant<128, false, false, false>, prepare_variant<128, true, true, false>,
+        prepare_variant<128, false, true, false>, prepare_variant<64, true, false, false>,   prepare_variant<64, false, false, false>,
+        prepare_variant<64, true, true, false>,   prepare_variant<64, false, true, false>,   prepare_variant<128, true, false, true>,
+        prepare_variant<128, false, false, true>, prepare_variant<128, true, true, true>,    prepare_variant<128, false, true, true>,
+        prepare_variant<64, true, false, true>,   prepare_variant<64, false, false, true>,   prepare_variant<64, true, true, true>,
+        prepare_variant<64, false, true, true>};
     for (const auto prepare : all) {
       const kv_status_t s = prepare();
       if (s != KV_OK) return s;
@@ -366,7 +389,7 @@ static kv_status_t resident_clusters(int device, int i, int* n) {
     cfg.attrs = attr + 1;
     cfg.numAttrs = 1;
     int clusters = 0;
-    if (cudaOccupancyMaxActiveClusters(&clusters, attn_decode_kernel<D, true, false>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&clusters, attn_decode_kernel<D, true, false, false>, &cfg) != cudaSuccess) {
       cudaGetLastError();
       clusters = 0;
     }
@@ -449,20 +472,24 @@ static bool few_pages(const kv_pool_t* p, int64_t blocks, int warps, int max_ctx
   return pages <= (p->head_dim == 64 ? 2.75 : blocks <= 2 * sm_count_of(p->device) ? 2.0 : 1.0);
 }
 
-template <int D, bool RING, bool MULTI>
+template <int D, bool RING, bool MULTI, bool SEL>
 static kv_status_t launch_decode_variant(const kv_pool_t* p, const DecodeArgs& a, int64_t blocks, cudaStream_t st) {
   const kv_status_t s = decode_setup(p->device);
   if (s != KV_OK) return s;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr[2];
   decode_config(cfg, attr, a.splits, blocks, decode_smem_bytes<D, RING>(), st);
-  KV_CUDA_OK(cudaLaunchKernelEx(&cfg, attn_decode_kernel<D, RING, MULTI>, a));
+  KV_CUDA_OK(cudaLaunchKernelEx(&cfg, attn_decode_kernel<D, RING, MULTI, SEL>, a));
   count_launch();
   return KV_OK;
 }
+template <int D, bool RING, bool SEL>
+static kv_status_t launch_decode_kernel(const kv_pool_t* p, const DecodeArgs& a, int64_t blocks, cudaStream_t st) {
+  return a.per_cta > 1 ? launch_decode_variant<D, RING, true, SEL>(p, a, blocks, st) : launch_decode_variant<D, RING, false, SEL>(p, a, blocks, st);
+}
 template <int D, bool RING>
 static kv_status_t launch_decode_kernel(const kv_pool_t* p, const DecodeArgs& a, int64_t blocks, cudaStream_t st) {
-  return a.per_cta > 1 ? launch_decode_variant<D, RING, true>(p, a, blocks, st) : launch_decode_variant<D, RING, false>(p, a, blocks, st);
+  return a.lists.pages != nullptr ? launch_decode_kernel<D, RING, true>(p, a, blocks, st) : launch_decode_kernel<D, RING, false>(p, a, blocks, st);
 }
 
 // What the entry points ask their callers for.  The kernel keeps its partial results on chip and uses none of it; the
@@ -476,12 +503,19 @@ size_t decode_workspace_bytes(int n_q_heads, int head_dim, int batch, int max_ct
   return align256(slots * head_dim * sizeof(float)) + align256(slots * sizeof(float));
 }
 
+// lists: the pages each (sequence, KV head) attends over, all of them without.
 // beside: the kernel may start while the kernel in front of it in the stream still runs and does not wait for it
 // (nothing it touches is written there).  The mixed step uses this to run decode next to the extend kernel.
 kv_status_t launch_decode(kv_pool_t* p, const void* q, int n_q_heads, const int* block_tables, int max_pages,
                           const int* ctx_lens, int batch, int max_ctx_len, float scale, void* out, float* lse,
-                          cudaStream_t st, bool beside) {
+                          cudaStream_t st, bool beside, const PageLists* lists) {
   DecodeArgs a{};
+  const int64_t bound = ((int64_t)max_ctx_len + kDecodeChunkTokens - 1) / kDecodeChunkTokens * kDecodeChunkTokens;
+  a.len_bound = (int)(bound < 0x7fffffffLL ? bound : 0x7fffffffLL);
+  if (lists != nullptr) {  // a pair's work is that of its list
+    a.lists = *lists;
+    if ((int64_t)lists->width * kPageSize < max_ctx_len) max_ctx_len = lists->width * kPageSize;
+  }
   a.pool = p->view();
   a.q = (const __nv_bfloat16*)q;
   a.block_tables = block_tables;
@@ -492,8 +526,6 @@ kv_status_t launch_decode(kv_pool_t* p, const void* q, int n_q_heads, const int*
   const kv_status_t s = p->head_dim == 128 ? decode_splits<128>(p, batch, max_ctx_len, &a.splits)
                                            : decode_splits<64>(p, batch, max_ctx_len, &a.splits);
   if (s != KV_OK) return s;
-  const int64_t bound = ((int64_t)max_ctx_len + kDecodeChunkTokens - 1) / kDecodeChunkTokens * kDecodeChunkTokens;
-  a.len_bound = (int)(bound < 0x7fffffffLL ? bound : 0x7fffffffLL);
   a.wait_mode = beside ? kWaitLast : kWaitFirst;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.out = (__nv_bfloat16*)out;

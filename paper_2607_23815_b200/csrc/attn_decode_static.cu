@@ -10,7 +10,7 @@ namespace kvattn {
 size_t decode_workspace_bytes(int n_q_heads, int head_dim, int batch, int max_ctx_len);
 kv_status_t launch_decode(kv_pool_t* p, const void* q, int n_q_heads, const int* block_tables, int max_pages,
                           const int* ctx_lens, int batch, int max_ctx_len, float scale, void* out, float* lse,
-                          cudaStream_t st, bool beside = false);
+                          cudaStream_t st, bool beside = false, const PageLists* lists = nullptr);
 
 constexpr size_t kStaticScratchBytes = size_t(8) << 20;
 }  // namespace kvattn

@@ -43,6 +43,37 @@ int size(const at::Tensor& t, int dim) {
   return (int)t.size(dim);
 }
 
+// What the calls around attention add to that: types and sizes, which a strided row would otherwise hide.
+const at::Tensor& typed(PyObject* o, at::ScalarType type) {
+  const at::Tensor& t = tensor(o);
+  if (t.scalar_type() != type) raise(PyExc_TypeError, type == at::kInt ? "expected an int32 tensor" : type == at::kFloat ? "expected a float32 tensor" : "expected a bfloat16 tensor");
+  return t;
+}
+void expect(bool ok, const char* what) {
+  if (!ok) raise(PyExc_ValueError, what);
+}
+int* ints(PyObject* o, int64_t n, const char* what) {  // (None: nullptr)
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = typed(o, at::kInt);
+  expect(t.numel() == n, what);
+  return written<int>(t);
+}
+const int* read_ints(PyObject* o, int64_t n, const char* what) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = typed(o, at::kInt);
+  expect(t.numel() == n, what);
+  return read<int>(t);
+}
+// bf16 [tokens][heads][head_dim], dense inside a token, any distance from token to token (a part of a fused projection's rows).
+const at::Tensor& rows(PyObject* o) {
+  if (!THPVariable_Check(o)) raise(PyExc_TypeError, "expected a torch tensor");
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_cuda()) raise(PyExc_AssertionError, "expected a CUDA tensor");
+  if (t.scalar_type() != at::kBFloat16) raise(PyExc_TypeError, "expected a bfloat16 tensor");
+  expect(t.dim() == 3 && (t.size(2) < 2 || t.stride(2) == 1) && (t.size(1) < 2 || t.stride(1) == t.size(2)), "rows must be [tokens][heads][head_dim], dense inside a token");
+  return t;
+}
+
 int integer(PyObject* o) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) throw Raised{};
@@ -226,6 +257,118 @@ PyObject* mixed(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+PyObject* step_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 12, [&] {
+    kv_pool_t* p = pool(a[0]);
+    const at::Tensor &ctx = typed(a[1], at::kInt), &fresh = typed(a[3], at::kInt), &bt = typed(a[4], at::kInt), &slots = typed(a[7], at::kInt);
+    const int64_t batch = ctx.numel(), total = slots.numel();
+    expect(bt.dim() == 2 && bt.size(0) == batch, "block_tables must have a row for each sequence");
+    const int* news = read_ints(a[2], batch, "new_lens must have an entry for each sequence");
+    int* cu = ints(a[5], batch + 1, "cu_new must have an entry for each sequence and one more");
+    int* pos = ints(a[6], total, "positions must have an entry for each slot");
+    int* next = ints(a[8], batch, "next_lens must have an entry for each sequence");
+    const int* cursor = read_ints(a[9], 1, "cursor must have one entry");
+    int* next_cursor = ints(a[10], 1, "next_cursor must have one entry");
+    const int *ctxp = read<int>(ctx), *freshp = read<int>(fresh);
+    int *btp = written<int>(bt), *slotp = written<int>(slots);
+    void* st = stream(a[11]);
+    const int pages = (int)fresh.numel(), width = size(bt, 1);
+    return unlocked([&] {
+      return kv_step_tables(p, ctxp, news, (int)batch, freshp, pages, btp, width, (int)total, cu, pos, slotp, next, cursor, next_cursor, st);
+    });
+  });
+}
+
+PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 13, [&] {
+    kv_pool_t* p = pool(a[0]);
+    const bool has_q = a[1] != Py_None, has_kv = a[2] != Py_None;
+    expect(has_kv == (a[3] != Py_None), "k_new and v_new go together");
+    expect(has_q || has_kv, "neither q nor k_new is given");
+    expect(has_q == (a[8] != Py_None), "q and q_out go together");
+    const at::Tensor &lead = rows(has_q ? a[1] : a[2]), &pos = typed(a[5], at::kInt), &freq = typed(a[6], at::kFloat);
+    const int64_t total = lead.size(0), dim = lead.size(2);
+    const void *q = nullptr, *k = nullptr, *v = nullptr;
+    void* out = nullptr;
+    int64_t qs = 0, ks = 0, vs = 0, os = 0;
+    int heads = 0;
+    if (has_q) {
+      const at::Tensor& o = rows(a[8]);
+      expect(o.sizes() == lead.sizes(), "q_out must have the shape of q");
+      q = read(lead), out = written(o), qs = lead.stride(0), os = o.stride(0), heads = size(lead, 1);
+    }
+    if (has_kv) {
+      const at::Tensor &kt = rows(a[2]), &vt = rows(a[3]);
+      expect(kt.sizes() == vt.sizes() && kt.size(0) == total && kt.size(2) == dim, "k_new and v_new must have the same shape, and q's tokens and head_dim");
+      expect(kt.size(1) == integer(a[10]) && dim == integer(a[11]), "k_new must have the pool's heads");
+      k = read(kt), v = read(vt), ks = kt.stride(0), vs = vt.stride(0);
+    }
+    expect(dim == integer(a[11]), "rows must have the pool's head_dim");
+    const int* slots = read_ints(a[4], total, "slots must have an entry for each token");
+    expect(pos.dim() >= 1 && pos.dim() <= 2 && pos.size(-1) == total, "positions must be [tokens] or [axes][tokens]");
+    const int axes = pos.dim() == 2 ? size(pos, 0) : 1, rot = 2 * (int)freq.numel();
+    const int* axis = read_ints(a[7], freq.numel(), "freq_axis must have an entry for each frequency");
+    const int* posp = read<int>(pos);
+    const float* freqp = read<float>(freq);
+    const int neighbours = integer(a[9]);
+    void* st = stream(a[12]);
+    return unlocked([&] {
+      return kv_append_rotary(p, q, qs, k, ks, v, vs, heads, slots, posp, axes, freqp, axis, rot, neighbours, (int)total, out, os, st);
+    });
+  });
+}
+
+PyObject* page_bounds(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 4, [&] {
+    kv_pool_t* p = pool(a[0]);
+    const at::Tensor &slots = typed(a[1], at::kInt), &bounds = typed(a[2], at::kBFloat16);
+    expect(bounds.nbytes() >= kv_page_bounds_bytes(p), "bounds must have kv_page_bounds_bytes() bytes");
+    const int* sp = read<int>(slots);
+    void *bp = written(bounds), *st = stream(a[3]);
+    const int total = (int)slots.numel();
+    return unlocked([&] { return kv_page_bounds(p, sp, total, bp, st); });
+  });
+}
+
+PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 12, [&] {
+    kv_pool_t* p = pool(a[0]);
+    const at::Tensor &q = typed(a[1], at::kBFloat16), &bounds = typed(a[2], at::kBFloat16), &bt = typed(a[3], at::kInt), &list = typed(a[8], at::kInt);
+    expect(q.dim() == 3 && bt.dim() == 2 && list.dim() == 3, "q must be [batch][heads][head_dim], block_tables [batch][pages], pages [batch][kv heads][n]");
+    const int64_t batch = q.size(0);
+    expect(bounds.nbytes() >= kv_page_bounds_bytes(p), "bounds must have kv_page_bounds_bytes() bytes");
+    expect(bt.size(0) == batch && list.size(0) == batch && list.size(1) == integer(a[11]), "block_tables and pages must have a row for each sequence, pages for each of the pool's heads");
+    const int* ctx = read_ints(a[4], batch, "ctx_lens must have an entry for each sequence");
+    int* counts = ints(a[9], batch * list.size(1), "counts must be [batch][kv heads]");
+    const int max_ctx = integer(a[5]), first = integer(a[6]), last = integer(a[7]), hq = size(q, 1), width = size(bt, 1), want = size(list, 2);
+    const void *qp = read(q), *bp = read(bounds);
+    const int* btp = read<int>(bt);
+    int* lp = written<int>(list);
+    void* st = stream(a[10]);
+    return unlocked([&] { return attn_select_pages(p, qp, hq, bp, btp, width, ctx, (int)batch, max_ctx, want, first, last, lp, counts, st); });
+  });
+}
+
+PyObject* decode_selected(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return call(n, 12, [&] {
+    kv_pool_t* p = pool(a[0]);
+    const at::Tensor &q = typed(a[1], at::kBFloat16), &bt = typed(a[2], at::kInt), &list = typed(a[5], at::kInt), &out = typed(a[8], at::kBFloat16), &lse = typed(a[9], at::kFloat);
+    expect(q.dim() == 3 && bt.dim() == 2 && list.dim() == 3, "q must be [batch][heads][head_dim], block_tables [batch][pages], pages [batch][kv heads][n]");
+    const int64_t batch = q.size(0);
+    expect(bt.size(0) == batch && list.size(0) == batch && list.size(1) == integer(a[11]), "block_tables and pages must have a row for each sequence, pages for each of the pool's heads");
+    expect(out.sizes() == q.sizes() && lse.numel() == batch * q.size(1), "out must have the shape of q, lse an entry for each of its rows");
+    const int* ctx = read_ints(a[3], batch, "ctx_lens must have an entry for each sequence");
+    const int* counts = read_ints(a[6], batch * list.size(1), "counts must be [batch][kv heads]");
+    const int max_ctx = integer(a[4]), hq = size(q, 1), pages = size(bt, 1), width = size(list, 2);
+    const float scale = real(a[7]);
+    const void* qp = read(q);
+    const int *btp = read<int>(bt), *lp = read<int>(list);
+    void *op = written(out), *st = stream(a[10]);
+    float* lsep = written<float>(lse);
+    return unlocked([&] { return attn_decode_selected(p, qp, hq, btp, pages, ctx, (int)batch, max_ctx, lp, counts, width, scale, op, lsep, st); });
+  });
+}
+
 const at::Tensor& host_tensor(PyObject* o) {
   if (!THPVariable_Check(o)) raise(PyExc_TypeError, "expected a torch tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
@@ -261,6 +404,11 @@ PyMethodDef methods[] = {ENTRY("kv_append", append),
                          ENTRY("attn_extend_planned", extend_planned),
                          ENTRY("attn_extend_shared", extend_shared),
                          ENTRY("attn_mixed", mixed),
+                         ENTRY("kv_step_tables", step_tables),
+                         ENTRY("kv_append_rotary", append_rotary),
+                         ENTRY("kv_page_bounds", page_bounds),
+                         ENTRY("attn_select_pages", select_pages),
+                         ENTRY("attn_decode_selected", decode_selected),
                          ENTRY("attn_extend_host", extend_host),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kvattn_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

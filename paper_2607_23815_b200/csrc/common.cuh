@@ -49,6 +49,13 @@ struct FanArgs {
   int n_children;
 };
 
+// The pages a decode call attends over: blocks of the sequence, by (sequence, KV head).
+struct PageLists {
+  const int* pages;   // [batch][n_kv_heads][width]
+  const int* counts;  // [batch][n_kv_heads]
+  int width;
+};
+
 extern std::atomic<int64_t> g_launches;
 inline void count_launch(int n = 1) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 

@@ -77,6 +77,12 @@ _SIGNATURES = {
     "attn_decode_static": (_I, [_P, _P, _I, _P, _I, _P, _I, _I, _F, _P, _P, _P]),
     "attn_decode_static_scratch_bytes": (_SZ, []),
     "attn_mixed": (_I, [_P, _I, _F, C.POINTER(ExtendArgs), C.POINTER(DecodeArgs), _P, _SZ, _P]),
+    "kv_step_tables": (_I, [_P, _P, _P, _I, _P, _I, _P, _I, _I, _P, _P, _P, _P, _P, _P, _P]),
+    "kv_append_rotary": (_I, [_P, _P, _I64, _P, _I64, _P, _I64, _I, _P, _P, _I, _P, _P, _I, _I, _I, _P, _I64, _P]),
+    "kv_page_bounds_bytes": (_SZ, [_P]),
+    "kv_page_bounds": (_I, [_P, _P, _I, _P, _P]),
+    "attn_select_pages": (_I, [_P, _P, _I, _P, _P, _I, _P, _I, _I, _I, _I, _I, _P, _P, _P]),
+    "attn_decode_selected": (_I, [_P, _P, _I, _P, _I, _P, _I, _I, _P, _P, _I, _F, _P, _P, _P]),
     "kv_check_batch": (_I, [_P, _P, _I, _P, _I, _P]),
     "kv_last_async_status": (_I, [_P]),
     "kvattn_set_extend_impl": (_I, [_I]),
@@ -360,6 +366,42 @@ def decode_args(q, block_tables, ctx_lens, max_ctx_len, out, lse) -> DecodeArgs:
 def attn_mixed(pool: Pool, n_q_heads, scale, ext: Optional[ExtendArgs], dec: Optional[DecodeArgs], workspace,
                stream=None):
     _check(_native.attn_mixed(pool.ptr, n_q_heads, scale, ext, dec, workspace, stream), "attn_mixed")
+
+
+def kv_step_tables(pool: Pool, ctx_lens, new_lens, new_pages, block_tables, cu_new, positions, slots, next_lens=None, cursor=None,
+                   next_cursor=None, stream=None):
+    """Block tables, positions and slots of a step's new tokens from the sequences' lengths (see the header).  slots has a row for
+    every token, and more if the step is padded; positions, next_lens, cursor and next_cursor may be None."""
+    _check(_native.kv_step_tables(pool.ptr, ctx_lens, new_lens, new_pages, block_tables, cu_new, positions, slots, next_lens, cursor,
+                                  next_cursor, stream), "kv_step_tables")
+
+
+def kv_append_rotary(pool: Pool, q, k_new, v_new, slots, positions, inv_freq, freq_axis, q_out, neighbours=False, stream=None):
+    """Rotates q into q_out and k_new into its slots by their positions ([tokens] or [axes][tokens]), stores v_new in its slots.  The
+    rows may lie apart (parts of a fused projection's output); q and q_out, or k_new and v_new, may be None; q_out may be q."""
+    _check(_native.kv_append_rotary(pool.ptr, q, k_new, v_new, slots, positions, inv_freq, freq_axis, q_out, int(neighbours),
+                                    pool.n_kv_heads, pool.head_dim, stream), "kv_append_rotary")
+
+
+def kv_page_bounds_bytes(pool: Pool) -> int:
+    return lib().kv_page_bounds_bytes(pool.handle)
+
+
+def kv_page_bounds(pool: Pool, slots, bounds, stream=None):
+    """Renews the bounds (bf16 [num_pages][n_kv_heads][2][head_dim]) of the pages that rows have been stored in, by their slots."""
+    _check(_native.kv_page_bounds(pool.ptr, slots, bounds, stream), "kv_page_bounds")
+
+
+def attn_select_pages(pool: Pool, q, bounds, block_tables, ctx_lens, max_ctx_len, n_first, n_last, pages, counts, stream=None):
+    """Writes, for every sequence and KV head, the pages.shape[2] pages that its query can have the largest scores with."""
+    _check(_native.attn_select_pages(pool.ptr, q, bounds, block_tables, ctx_lens, max_ctx_len, n_first, n_last, pages, counts, stream,
+                                     pool.n_kv_heads), "attn_select_pages")
+
+
+def attn_decode_selected(pool: Pool, q, block_tables, ctx_lens, max_ctx_len, pages, counts, scale, out, lse, stream=None):
+    """attn_decode over the listed pages of each sequence and KV head."""
+    _check(_native.attn_decode_selected(pool.ptr, q, block_tables, ctx_lens, max_ctx_len, pages, counts, scale, out, lse, stream,
+                                        pool.n_kv_heads), "attn_decode_selected")
 
 
 def kv_check_batch(pool: Pool, block_tables, lens, stream=None) -> int:
