@@ -105,7 +105,11 @@ static cudaError_t launch_bounds(const kv_pool_t* p, const int* slots, int total
   int tile = 1;
   while (tile < 32 && (int64_t)total * p->n_kv_heads >= (int64_t)2 * tile * sms * 32) tile *= 2;
   const int64_t units = (int64_t)((total + tile - 1) / tile) * p->n_kv_heads, want = (units + kBoundsWarps - 1) / kBoundsWarps, most = (int64_t)sms * 16;
-  return launch_early(page_bounds_kernel<D>, (unsigned)(want < most ? want : most), kBoundsWarps * 32, 0, st, p->view(), slots, total, tile, (uint4*)bounds);
+  static std::atomic<bool> allowed[kMaxDevices];
+  const int smem = few_blocks_smem(want, sms);
+  return launch_early(page_bounds_kernel<D>, (unsigned)(want < most ? want : most), kBoundsWarps * 32,
+                      smem > 0 && allow_smem((const void*)page_bounds_kernel<D>, spread_smem(1), allowed, p->device) ? smem : 0, st, p->view(), slots, total,
+                      tile, (uint4*)bounds);
 }
 
 }  // namespace kvattn

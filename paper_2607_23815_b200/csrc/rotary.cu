@@ -7,6 +7,11 @@
 // What bounds it: HBM on steps of many tokens (every row is read once and written once), latency on small ones.  A warp takes eight (D = 64:
 // sixteen) rows of a token, whatever mixture of queries, keys and values they are, and each lane the two 16-byte chunks whose dims pair
 // up, so that a pair never leaves its lane; the lanes that hold the same dims of different rows share out the sines and cosines.
+// 10123 tokens, 32/8 heads of 128, parts of one projection: 40.5 us, 6.1 TB/s of the 248 MB (copy rate 6.55); 9 x 300-2000, heads of 64, three axes:
+// 25.7 us, 5.6 TB/s; one token 2.5 us.
+// Four blocks of eight warps to an SM (64 registers), which walk the units in one grid's strides: three blocks 41.4 us, more blocks than are resident
+// 42.9, all rows of a token to a warp (one set of sines for six units) 44.8, runs of neighbouring units to a warp 49.8, twice the rows in flight per
+// warp with three blocks 42.1.
 #include "common.cuh"
 #include "page_mma.cuh"
 #include "sm100_ptx.cuh"
@@ -28,9 +33,10 @@ struct RotaryArgs {
 
 constexpr int kRotaryWarps = 8;
 constexpr int kRotaryPasses = 2;
+constexpr int kRotaryBlocks = 4;  // on an SM
 
 template <int D>
-__global__ void __launch_bounds__(kRotaryWarps * 32) append_rotary_kernel(const RotaryArgs a) {
+__global__ void __launch_bounds__(kRotaryWarps * 32, kRotaryBlocks) append_rotary_kernel(const RotaryArgs a) {
   constexpr int kLanes = D / 16;          // of a row: a pair of chunks each
   constexpr int kRows = 32 / kLanes;      // of a pass
   constexpr int kShare = 8 / kRows;       // frequencies of which a lane takes the sine and cosine
@@ -59,10 +65,10 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) append_rotary_kernel(const 
     }
   }
 
-  const int64_t units = (int64_t)a.total * a.slices;
+  const unsigned units = (unsigned)a.total * a.slices;
   bool let_in = false;
-  for (int64_t u = (int64_t)blockIdx.x * kRotaryWarps + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * kRotaryWarps) {
-    const int t = (int)(u / a.slices), row0 = (int)(u - (int64_t)t * a.slices) * (kRows * kRotaryPasses) + g;
+  for (unsigned u = blockIdx.x * kRotaryWarps + (threadIdx.x >> 5); u < units; u += gridDim.x * kRotaryWarps) {
+    const int t = (int)(u / (unsigned)a.slices), slice = (int)(u - (unsigned)t * a.slices), row0 = slice * (kRows * kRotaryPasses) + g;
     // the rows first: everything else is found while they are on their way
     uint4 x[kRotaryPasses][2];
 #pragma unroll
@@ -99,6 +105,7 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) append_rotary_kernel(const 
       ptx::launch_dependents();
       let_in = true;
     }
+    const bool clears = follow != slot + 1;  // the last row of its page clears the slots behind it, as kv_append's does
     if (slot < 0) continue;  // a padding row: nothing of it is written
     const int page = slot / kPageSize, at = slot % kPageSize;
     if (page >= a.pool.num_pages) {
@@ -141,24 +148,38 @@ __global__ void __launch_bounds__(kRotaryWarps * 32) append_rotary_kernel(const 
         char* base = reinterpret_cast<char*>(is_v ? a.pool.v : a.pool.k) + ((size_t)page * a.n_kv + head) * blk;
         *reinterpret_cast<uint4*>(base + chunk_offset_bytes(at, c0, D)) = x[i][0];
         *reinterpret_cast<uint4*>(base + chunk_offset_bytes(at, c1, D)) = x[i][1];
-        if (follow != slot + 1) {  // the last row of its page clears the slots behind it, as kv_append's does
-          const uint4 z = make_uint4(0, 0, 0, 0);
-          for (int s = at + 1; s < kPageSize; ++s) {
-            *reinterpret_cast<uint4*>(base + chunk_offset_bytes(s, c0, D)) = z;
-            *reinterpret_cast<uint4*>(base + chunk_offset_bytes(s, c1, D)) = z;
-          }
+      }
+    }
+    // The slots behind are shared out over the token's units: they can be fifteen times what the token itself takes, and in the units that hold its
+    // keys and values alone they were the longest part of a decode step (40 tokens 4.2 us, this way 3.5; 256 5.8 and 5.2).
+    if (clears) {
+      constexpr int kChunks = D / 8;  // of a row
+      for (int s = at + 1 + slice; s < kPageSize; s += a.slices) {
+        const size_t off = ((size_t)page * a.n_kv + lane / kChunks) * blk + chunk_offset_bytes(s, lane % kChunks, D);
+        char *kp = reinterpret_cast<char*>(a.pool.k) + off, *vp = reinterpret_cast<char*>(a.pool.v) + off;
+#pragma unroll 4
+        for (int head = lane / kChunks; head < a.n_kv; head += 32 / kChunks, kp += 32 / kChunks * blk, vp += 32 / kChunks * blk) {
+          *reinterpret_cast<uint4*>(kp) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(vp) = make_uint4(0, 0, 0, 0);
         }
       }
     }
   }
 }
 
+static int rotary_slices(int head_dim, int rows) {
+  const int step = 32 / (head_dim / 16) * kRotaryPasses;
+  return (rows + step - 1) / step;
+}
+
 template <int D>
-static cudaError_t launch_rotary(const kv_pool_t* p, RotaryArgs& a, cudaStream_t st) {
-  const int per_unit = 32 / (D / 16) * kRotaryPasses;
-  a.slices = (a.n_q + 2 * a.n_kv + per_unit - 1) / per_unit;
-  const int64_t want = ((int64_t)a.total * a.slices + kRotaryWarps - 1) / kRotaryWarps, most = (int64_t)sm_count_of(p->device) * 16;
-  return launch_early(append_rotary_kernel<D>, (unsigned)(want < most ? want : most), kRotaryWarps * 32, 0, st, a);
+static cudaError_t launch_rotary(const kv_pool_t* p, const RotaryArgs& a, cudaStream_t st) {
+  static std::atomic<bool> allowed[kMaxDevices];
+  const int sms = sm_count_of(p->device);
+  const int64_t want = ((int64_t)a.total * a.slices + kRotaryWarps - 1) / kRotaryWarps, most = (int64_t)sms * kRotaryBlocks;
+  const int smem = few_blocks_smem(want, sms);
+  return launch_early(append_rotary_kernel<D>, (unsigned)(want < most ? want : most), kRotaryWarps * 32,
+                      smem > 0 && allow_smem((const void*)append_rotary_kernel<D>, spread_smem(1), allowed, p->device) ? smem : 0, st, a);
 }
 
 }  // namespace kvattn
@@ -184,9 +205,11 @@ extern "C" kv_status_t kv_append_rotary(kv_pool_t* p, const void* q, int64_t q_s
   for (const auto& r : rows)
     if (r.heads > 0 && ((((uintptr_t)r.at) & 15) != 0 || (total_new > 1 && (r.stride % 8 != 0 || r.stride < (int64_t)r.heads * D))))
       return KV_ERR_INVALID;
+  const int slices = rotary_slices(D, n_q + 2 * n_kv);
+  if ((int64_t)total_new * slices > 0x7fffffffLL) return KV_ERR_UNSUPPORTED;
   if (!on_pool_device(p)) return KV_ERR_INVALID;
-  RotaryArgs a{p->view(), (const __nv_bfloat16*)q, (const __nv_bfloat16*)k_new, (const __nv_bfloat16*)v_new, q_stride, k_stride, v_stride,
-               q_out_stride, (__nv_bfloat16*)q_out, slots, positions, inv_freq, freq_axis, n_q, n_kv, n_axes, rot_dim, neighbours != 0, total_new, 0};
+  const RotaryArgs a{p->view(), (const __nv_bfloat16*)q, (const __nv_bfloat16*)k_new, (const __nv_bfloat16*)v_new, q_stride, k_stride, v_stride,
+               q_out_stride, (__nv_bfloat16*)q_out, slots, positions, inv_freq, freq_axis, n_q, n_kv, n_axes, rot_dim, neighbours != 0, total_new, slices};
   KV_CUDA_OK(D == 128 ? launch_rotary<128>(p, a, (cudaStream_t)stream) : launch_rotary<64>(p, a, (cudaStream_t)stream));
   count_launch();
   return KV_OK;

@@ -59,6 +59,13 @@ inline AppendSpread append_spread(int total_new, int chunks, int sms) {
   return {(int)blocks, (int)warps, held ? spread_smem((int)k) : shared, held ? shared : 0};
 }
 
+// Shared memory for each of `blocks` blocks of a kernel that is launched early, so that they are laid over the SMs and not packed onto a few: as many
+// to an SM as are its share, up to three, and room for as many of another stream's (see append_spread); 0 where there are more.
+inline int few_blocks_smem(int64_t blocks, int sms) {
+  const int64_t k = (blocks + sms - 1) / sms;
+  return k > 3 ? 0 : spread_smem(k == 1 && 2 * blocks > sms ? 2 : (int)k);
+}
+
 // Tokens of a block of the prologue that builds the plan beside the append: one block takes the plan, the others share the tokens,
 // up to 32 (the block's warps) each.
 inline int prologue_tokens(int total_new, int sms) {
