@@ -34,10 +34,10 @@ struct DecodeArgs {
   int per_cta;       // pairs a CTA takes, kWarps / per_cta warps each (1 where splits > 1)
   int len_bound;     // host-side bound on ctx_lens, up to a multiple of kDecodeChunkTokens (a longer sequence is reported and skipped)
   int wait_mode;     // kWaitFirst / kWaitLast
-  PageLists lists;   // the pages to attend over (SEL)
   float scale_log2;  // scale * log2(e)
   __nv_bfloat16* out;
   float* lse;
+  PageLists lists;   // the pages to attend over (SEL)
 };
 constexpr int kDecodeChunkTokens = 1024;
 constexpr int kWaitFirst = 0;  // everything queued before this kernel is waited for before anything is read

@@ -3,14 +3,18 @@
 // score(page) = max over the group's query heads of sum_d (q_d >= 0 ? q_d hi_d : q_d lo_d): no key of the page can have a larger product with any of
 // those heads.  Chosen are the n_first first and n_last last pages and those others that score highest, ties to the lowest index.
 //
-// The order is that of the scores as defined, not of a rounded sum.  Scores are first summed in 32 bits, with an error of at most `err` (below);
+// The order is that of the scores as defined, not of a rounded sum.  Scores are first summed by the tensor cores, with an error of at most `err` (below);
 // if the last page chosen and the best one left are further apart than two errors, no rounding has decided anything.  If not (a few rows in a hundred
 // of normal data, and wherever scores are equal, infinite or not numbers), the pages within two errors of the border are scored again in 64 bits, in
 // which the products of bf16 values are exact, and the choice is made among them.
 //
 // What bounds it: HBM (4 D bytes a page and KV head, read once) where there are many rows, latency where there are few, so a row's pages are then
-// shared out over a cluster whose CTAs push their scores into the shared memory of the first, which chooses.
+// shared out over a cluster whose CTAs push their scores into the shared memory of the first, which chooses.  A score is a product of (q+, q-), the
+// positive and the negative part of q, with (hi, lo): sixteen pages by eight heads in an mma.sync.m16n8k16 whose A fragments are the 16-byte chunks as
+// they lie.
 #include <math.h>
+
+#include <type_traits>
 
 #include "common.cuh"
 #include "page_mma.cuh"
@@ -28,187 +32,129 @@ struct SelectArgs {
   int* pages;                   // [batch][Hkv][n_select]
   int* counts;                  // [batch][Hkv]
   int max_pages, bound_pages;   // bound_pages: the keys there is shared memory for
-  int n_q_heads, n_select, n_first, n_last, splits;
+  int group, n_select, n_first, n_last, splits;
 };
 
-constexpr int kSelWarps = 8;
-constexpr int kSelThreads = kSelWarps * 32;
 constexpr int kSelMaxSplits = 8;
-constexpr int kSelMaxPages = 24576;  // 192 KB of keys
+constexpr int kSelMaxWarps = 16;
+constexpr int kSelMaxPages = 24576;  // 198 KB of keys and marks
 constexpr int kBins = 256;
 typedef unsigned long long u64;
 
-// Keys in the order of the values, whatever is not a number above all of them; -0 and 0 are the same.
+// Keys in the order of the values, whatever is not a number above all of them; -0 and 0 are the same.  A page has room for 64 bits in shared memory:
+// the sum of 32 bits takes the upper half, the exact score all of it.
 __device__ __forceinline__ uint32_t key_of(float x) {
-  if (isnan(x)) return 0xffffffffu;
   const uint32_t b = x == 0.f ? 0u : __float_as_uint(x);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  return isnan(x) ? 0xffffffffu : b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+__device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+constexpr u64 kBelow = 0, kAbove = ~0ull;  // keys of no value
 __device__ __forceinline__ u64 key_of(double x) {
-  if (isnan(x)) return ~0ull;
+  if (isnan(x)) return kAbove - 1;
   const u64 b = x == 0.0 ? 0ull : (u64)__double_as_longlong(x);
   return b >> 63 ? ~b : b | (1ull << 63);
 }
+template <typename Key>
+__device__ __forceinline__ Key key_at(const u64* keys, int i) {
+  if constexpr (sizeof(Key) == 4) return reinterpret_cast<const uint32_t*>(keys)[2 * i + 1];
+  else return keys[i];
+}
 
 struct SelectShared {
-  u64 lo, hi;                  // range of the keys still in question
-  u64 warp_lo[kSelWarps], warp_hi[kSelWarps];
-  unsigned hist[kBins];
-  int need, bin;
-  int warp_ge[kSelWarps], warp_eq[kSelWarps];
-  uint32_t bmax[kSelMaxSplits];  // largest magnitude among the bounds each CTA has read (bf16 bits)
-  uint32_t warp_bmax[kSelWarps];
-  float qsum;
+  uint4 q[2][4][32];  // [negative, positive elements][16-byte chunk 4 j + c of head r, by j][lane (r, c)]
+  float qsum[kSelMaxWarps];
+  unsigned hist[3][kBins];
+  // of each run of pages: the smallest and the largest key, the largest sum of magnitudes of a score's terms (bits)
+  uint32_t run_lo[kSelMaxSplits * kSelMaxWarps], run_hi[kSelMaxSplits * kSelMaxWarps], run_reach[kSelMaxSplits * kSelMaxWarps];
+  uint32_t warp_kept[kSelMaxWarps], warp_left[kSelMaxWarps];
+  u64 warp_lo[kSelMaxWarps], warp_hi[kSelMaxWarps];
+  int warp_above[kSelMaxWarps];
 };
 
-// The `need` largest of keys[0 .. m) are those >= ge and the first `eq` of those that equal ge - 1.
+// The chosen of the keys are those >= ge and the first `eq` of those that equal ge - 1.
 struct Choice {
   u64 ge;
   int eq;
 };
-
-__device__ __forceinline__ u64 warp_min(u64 v) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v = min(v, (u64)__shfl_xor_sync(0xffffffffu, v, off));
-  return v;
-}
-__device__ __forceinline__ u64 warp_max(u64 v) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v = max(v, (u64)__shfl_xor_sync(0xffffffffu, v, off));
-  return v;
-}
-
-// Smallest of the threads' lo and largest of their hi, for all of them.
-__device__ __forceinline__ void block_range(SelectShared& sh, u64& lo, u64& hi) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  lo = warp_min(lo);
-  hi = warp_max(hi);
-  __syncthreads();  // (the arrays may still be read for the range before)
-  if (lane == 0) {
-    sh.warp_lo[warp] = lo;
-    sh.warp_hi[warp] = hi;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kSelWarps; ++w) {
-    lo = min(lo, sh.warp_lo[w]);
-    hi = max(hi, sh.warp_hi[w]);
-  }
-}
-
-// By the bits of the keys, eight at a time, counted from the highest in which the keys in question differ; 1 <= need <= m.
-__device__ __forceinline__ Choice choose(SelectShared& sh, const u64* keys, int m, int need) {
-  const int tid = threadIdx.x, lane = tid & 31;
-  u64 lo = ~0ull, hi = 0;
-  for (int i = tid; i < m; i += kSelThreads) {
-    lo = min(lo, keys[i]);
-    hi = max(hi, keys[i]);
-  }
-  block_range(sh, lo, hi);
-  while (lo < hi) {
-    const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - 8);
-    for (int b = tid; b < kBins; b += kSelThreads) sh.hist[b] = 0;
-    __syncthreads();
-    for (int i = tid; i < m; i += kSelThreads) {
-      const u64 k = keys[i];
-      if (k >= lo && k <= hi) atomicAdd(&sh.hist[(unsigned)((k - lo) >> shift)], 1u);
-    }
-    __syncthreads();
-    if (tid < 32) {  // the bin that the last one needed lies in: lane 31 has the highest eight bins
-      unsigned mine[kBins / 32], sum = 0;
-#pragma unroll
-      for (int i = 0; i < kBins / 32; ++i) {
-        mine[i] = sh.hist[lane * (kBins / 32) + i];
-        sum += mine[i];
-      }
-      unsigned above = sum;  // then: in this lane's bins and those above
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const unsigned x = __shfl_down_sync(0xffffffffu, above, off);
-        if (lane + off < 32) above += x;
-      }
-      above -= sum;
-      if (above < (unsigned)need && above + sum >= (unsigned)need) {
-#pragma unroll
-        for (int i = kBins / 32 - 1; i >= 0; --i) {
-          if (above + mine[i] >= (unsigned)need) {
-            sh.bin = lane * (kBins / 32) + i;
-            sh.need = need - above;
-            break;
-          }
-          above += mine[i];
-        }
-      }
-    }
-    __syncthreads();
-    const u64 start = lo + ((u64)sh.bin << shift);
-    need = sh.need;
-    if (sh.hist[sh.bin] == (unsigned)need) return Choice{start, 0};
-    if (hi - start >= 1ull << shift) hi = start + ((1ull << shift) - 1);
-    lo = start;
-    __syncthreads();  // (bin, need and the counts are read before they are written again)
-  }
-  return Choice{lo + 1, need};  // all that is left is equal (lo = ~0: ge wraps to 0, see taken())
-}
-
-// Is a key among the chosen for sure / one of the equals of which only some are?  (Keys of ~0 make ge wrap around to 0.)
-__device__ __forceinline__ bool surely(const Choice& c, u64 k) { return c.ge == 0 && c.eq > 0 ? false : k >= c.ge; }
+__device__ __forceinline__ bool surely(const Choice& c, u64 k) { return k >= c.ge; }
 __device__ __forceinline__ bool equals(const Choice& c, u64 k) { return c.eq > 0 && k == c.ge - 1; }
 
-// Sum over kLanes neighbouring lanes of each of v[0 .. N): the lanes share out the sums; returns the largest of the N.
-template <int N, int kLanes>
-__device__ __forceinline__ float largest_sum(float (&v)[N]) {
-  const int lane = threadIdx.x & 31;
-  int n = N;
-#pragma unroll
-  for (int off = kLanes / 2; off > 0; off >>= 1) {
-    if (n > 1) {
-      n >>= 1;
-      const bool up = lane & off;
-#pragma unroll
-      for (int i = 0; i < N / 2; ++i)
-        if (i < n) {
-          const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
-          v[i] = keep + __shfl_xor_sync(0xffffffffu, give, off);
-        }
-    } else {
-      v[0] += __shfl_xor_sync(0xffffffffu, v[0], off);
+// The `need` largest of the keys in [lo, hi], by their bits, eight at a time, counted from the highest in which lo and hi differ; there are `need` of
+// them at least, 1 <= need.  One barrier a turn: every warp looks through the counts by itself, and there are three sets of them, so that the one that
+// is cleared for the next turn has been read by all.  turn: of the block's turns so far; set turn % 3 is clear.
+template <typename Key>
+__device__ __forceinline__ Choice choose(SelectShared& sh, const u64* keys, int m, int need, Key lo, Key hi, int& turn) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  while (lo < hi) {
+    const Key span = hi - lo;
+    const int bits = sizeof(Key) == 4 ? 32 - __clz((int)span) : 64 - __clzll((long long)span), shift = bits > 8 ? bits - 8 : 0;
+    unsigned* hist = sh.hist[turn % 3];
+    unsigned* next = sh.hist[(turn + 1) % 3];
+    ++turn;
+    for (int b = tid; b < kBins; b += blockDim.x) next[b] = 0;
+    for (int i = tid; i < m; i += blockDim.x) {
+      const Key k = key_at<Key>(keys, i);
+      if (k >= lo && k <= hi) atomicAdd(&hist[(unsigned)((k - lo) >> shift)], 1u);
     }
-  }
-  float best = v[0];
+    __syncthreads();
+    // the bin that the last one needed lies in: lane 31 has the highest eight bins
+    const uint4 h0 = *reinterpret_cast<const uint4*>(hist + 8 * lane), h1 = *reinterpret_cast<const uint4*>(hist + 8 * lane + 4);
+    const unsigned h[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w};
+    const unsigned sum = h[0] + h[1] + h[2] + h[3] + h[4] + h[5] + h[6] + h[7];
+    unsigned above = sum;  // then: in the bins above this lane's
 #pragma unroll
-  for (int off = kLanes / 2, k = N; k > 1; off >>= 1, k >>= 1) {
-    const float other = __shfl_xor_sync(0xffffffffu, best, off);
-    best = isnan(best) || best > other ? best : other;
+    for (int off = 1; off < 32; off <<= 1) {
+      const unsigned x = __shfl_down_sync(0xffffffffu, above, off);
+      if (lane + off < 32) above += x;
+    }
+    above -= sum;
+    unsigned bin = 0, count = 0, rest = 0;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+      if (above < (unsigned)need && above + h[i] >= (unsigned)need) {
+        bin = 8 * lane + i;
+        count = h[i];
+        rest = need - above;
+      }
+      above += h[i];
+    }
+    const int at = __ffs(__ballot_sync(0xffffffffu, count != 0)) - 1;
+    bin = __shfl_sync(0xffffffffu, bin, at);
+    count = __shfl_sync(0xffffffffu, count, at);
+    need = __shfl_sync(0xffffffffu, rest, at);
+    const Key start = lo + ((Key)bin << shift);
+    if (count == (unsigned)need) return Choice{start, 0};
+    if ((Key)(hi - start) >> shift != 0) hi = start + (((Key)1 << shift) - 1);
+    lo = start;
   }
-  return best;
+  return Choice{(u64)lo + 1, need};  // all that is left is equal
 }
-
-template <int kDims>
-__device__ __forceinline__ void load_dims(uint32_t (&w)[kDims / 2], const __nv_bfloat16* p) {
-  if constexpr (kDims == 8)
-    asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
-  else
-    asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-}
-__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 // The score by its definition, in 64 bits, for the whole warp.
-template <int D, int G>
-__device__ __forceinline__ u64 exact_key(const __nv_bfloat16* q, const __nv_bfloat16* bounds) {
-  constexpr int kDims = D / 32;
+template <int D>
+__device__ __forceinline__ u64 exact_key(const __nv_bfloat16* q, const __nv_bfloat16* bounds, int group) {
+  constexpr int kDims = D / 32, kWords = kDims / 2;  // of a lane
   const int lane = threadIdx.x & 31;
+  auto load = [&](const __nv_bfloat16* p, uint32_t (&w)[kWords]) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = (uint32_t)ptx::ld_plain(reinterpret_cast<const int*>(p + lane * kDims) + i);
+  };
+  auto value = [](const uint32_t (&w)[kWords], int i) { return (double)__uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); };
+  uint32_t lo[kWords], hi[kWords], x[8][kWords];
+  load(bounds, lo);
+  load(bounds + D, hi);
+#pragma unroll
+  for (int g = 0; g < 8; ++g)
+    if (g < group) load(q + g * D, x[g]);
   double best = -INFINITY;
-#pragma unroll 1
-  for (int g = 0; g < G; ++g) {
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    if (g >= group) break;
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < kDims; ++i) {
-      const int d = lane * kDims + i;
-      const double x = (double)__bfloat162float(q[g * D + d]);
-      sum += x * (double)__bfloat162float(x >= 0.0 ? bounds[D + d] : bounds[d]);
+      const double v = value(x[g], i);
+      sum += v * (v >= 0.0 ? value(hi, i) : value(lo, i));
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
@@ -217,135 +163,168 @@ __device__ __forceinline__ u64 exact_key(const __nv_bfloat16* q, const __nv_bflo
   return key_of(best);
 }
 
-template <int D, int G>
-__global__ void __launch_bounds__(kSelThreads) select_pages_kernel(const SelectArgs a) {
-  constexpr int kDims = G == 8 ? 4 : 8;      // of a lane (its q takes 2 G kDims registers)
-  constexpr int kLanes = D / kDims;          // of a page
-  constexpr int kAtOnce = 32 / kLanes;       // pages of a warp's load
-  constexpr int kDeep = 4;                   // loads in flight
+template <int D, int kWarps>
+__global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(const SelectArgs a) {
+  constexpr int NJ = D / 32;  // 16-byte chunks of lo (and of hi) of a page that a lane takes
+  constexpr int kThreads = kWarps * 32;
   extern __shared__ u64 keys[];
-  __shared__ SelectShared sh;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, sub = lane / kLanes, dim0 = lane % kLanes * kDims;
+  __shared__ __align__(16) SelectShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int splits = a.splits, row = blockIdx.x / splits, rank = blockIdx.x - row * splits;
-  const int Hkv = a.pool.n_kv_heads, seq = row / Hkv, kvh = row - seq * Hkv;
+  const int Hkv = a.pool.n_kv_heads, G = a.group, seq = row / Hkv, kvh = row - seq * Hkv;
+  const int runs = kWarps * splits, run = rank * kWarps + warp;
+  for (int b = tid; b < kBins; b += kThreads) sh.hist[0][b] = 0;
   if (splits > 1) cluster_arrive();
   ptx::dependency_wait();
 
+  // The length, the first pages and the query at once; what the length rules out is not used.  A warp takes every `runs`-th sixteen pages, the next two
+  // sixteens' ids are on their way meanwhile.
   const int L = ptx::ld_plain(a.ctx_lens + seq);
+  const int* table = a.block_tables + (int64_t)seq * a.max_pages + a.n_first;
+  auto table_entry = [&](int tile, int limit) {  // lanes 0 - 15: of this sixteen, 16 - 31: of the warp's next
+    const int i = (tile + (lane >> 4) * runs) * 16 + (lane & 15);
+    return i < limit ? ptx::ld_plain(table + i) : 0;
+  };
+  const int in_table = min(a.max_pages, a.bound_pages) - a.n_first;
+  int ids = table_entry(run, in_table), ids_behind = table_entry(run + 2 * runs, in_table);
+  const __nv_bfloat16* q = a.q + ((int64_t)seq * Hkv + kvh) * G * D;
+  static_assert(kWarps >= NJ, "a warp for every chunk of the query");
+  if (warp < NJ) {  // head r's chunks 4 warp + c: the positive elements (for hi) and the others (for lo)
+    const uint4 x = r < G ? ptx::ld_plain(reinterpret_cast<const uint4*>(q + r * D) + 4 * warp + c) : make_uint4(0, 0, 0, 0);
+    uint4 pos, neg;
+    float sum = 0.f;
+    bool odd = false;  // an element below the normal numbers, which the tensor cores may take for 0
+    auto split = [&](uint32_t w, uint32_t& pos, uint32_t& neg) {
+      const uint32_t mask = (w & 0x8000u ? 0xffffu : 0u) | (w & 0x80000000u ? 0xffff0000u : 0u);
+      pos = w & ~mask;
+      neg = w & mask;
+      sum += fabsf(__uint_as_float(w << 16)) + fabsf(__uint_as_float(w & 0xffff0000u));
+      odd |= ((w & 0x7f80u) == 0 && (w & 0x7fu) != 0) || ((w & 0x7f800000u) == 0 && (w & 0x7f0000u) != 0);
+    };
+    split(x.x, pos.x, neg.x);
+    split(x.y, pos.y, neg.y);
+    split(x.z, pos.z, neg.z);
+    split(x.w, pos.w, neg.w);
+    sh.q[0][warp][lane] = neg;
+    sh.q[1][warp][lane] = pos;
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    sum = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sum)));  // (not a number: above all)
+    if (__any_sync(0xffffffffu, odd)) sum = INFINITY;
+    if (lane == 0) sh.qsum[warp] = sum;
+  }
+
   const bool fits = L <= a.max_pages * (int64_t)kPageSize && L <= a.bound_pages * (int64_t)kPageSize;
   if (!fits && rank == 0 && tid == 0) report(a.pool.status, KV_ERR_BOUNDS);  // left unwritten
   const int nb = fits && L > 0 ? (int)(((int64_t)L + kPageSize - 1) / kPageSize) : 0;
   int* list = a.pages + (int64_t)row * a.n_select;
-  if (nb <= a.n_select) {  // every page is chosen
-    if (splits > 1) cluster_wait();
-    if (fits && rank == 0) {
-      for (int i = tid; i < a.n_select; i += kSelThreads) list[i] = i < nb ? i : -1;
-      if (tid == 0) a.counts[row] = nb;
-    }
-    return;
-  }
-
-  // ---- scores of the pages n_first .. nb - n_last - 1; key i is that of page n_first + i
-  const int m = nb - a.n_first - a.n_last, need = a.n_select - a.n_first - a.n_last;
-  const __nv_bfloat16* q = a.q + ((int64_t)seq * a.n_q_heads + kvh * G) * D;
-  const int* table = a.block_tables + (int64_t)seq * a.max_pages + a.n_first;
+  const int m = nb - a.n_first - a.n_last, need = a.n_select - a.n_first - a.n_last;  // key i is that of page n_first + i
   const int64_t page_stride = (int64_t)Hkv * 2 * D;
   const __nv_bfloat16* base = a.bounds + (int64_t)kvh * 2 * D;
-  if (need > 0) {
-    const int runs = kSelWarps * splits, run = rank * kSelWarps + warp;
-    const int begin = (int)((int64_t)m * run / runs), end = (int)((int64_t)m * (run + 1) / runs);
-    auto table_entry = [&](int i) {
-      int pg = 0;
-      if (i < end) {
-        pg = ptx::ld_plain(table + i);
-        if ((unsigned)pg >= (unsigned)a.pool.num_pages) {
+  const bool all = nb <= a.n_select, scored = !all && need > 0;
+
+  // ---- scores
+  if (scored) {
+    if (splits > 1) cluster_wait();  // the first CTA runs: its shared memory may be written
+    const uint32_t keys0 = ptx::smem_u32(keys), keys_at = splits > 1 ? cluster_addr(keys0, 0) : keys0;
+    uint32_t reach = 0, least = 0xffffffffu, most = 0;  // reach: the largest sum of the magnitudes of a score's terms (bits)
+    const int tiles = (m + 15) / 16;
+    // A tile's two pages of this lane.  While one half of a tile (lo, then hi) is multiplied, the other one and the same half of the next tile are on
+    // their way.
+    const uint4* src[2];
+    bool in[2];
+    auto find = [&](int n, int tile) {  // the n-th tile of the warp, each once and in order
+      if ((n & 1) == 0 && n > 0) {
+        ids = ids_behind;
+        ids_behind = table_entry(tile + 2 * runs, m);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        int pg = __shfl_sync(0xffffffffu, ids, 16 * (n & 1) + 8 * s + r);
+        in[s] = 16 * tile + 8 * s + r < m;
+        if (in[s] && (unsigned)pg >= (unsigned)a.pool.num_pages) {
           report(a.pool.status, KV_ERR_BOUNDS);
           pg = 0;  // stay inside; the result of this row is flagged, not trusted
         }
+        src[s] = reinterpret_cast<const uint4*>(base + pg * page_stride) + c;
       }
-      return pg;
     };
-    int cur = table_entry(begin + lane), nxt = table_entry(begin + 32 + lane), at = begin;
-    float qp[G][kDims], qn[G][kDims], qsum = 0.f;
+    typedef uint4 Half[2][NJ];
+    auto load = [&](Half& x, int at) {
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      uint32_t w[kDims / 2];
-      load_dims<kDims>(w, q + g * D + dim0);
-      float sum = 0.f;
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int i = 0; i < kDims; ++i) {
-        const float x = i & 1 ? high_half(w[i / 2]) : low_half(w[i / 2]);
-        qp[g][i] = x >= 0.f ? x : 0.f;
-        qn[g][i] = x >= 0.f ? 0.f : x;  // (not a number: here, and so in every score)
-        sum += fabsf(x);
+        for (int j = 0; j < NJ; ++j) x[s][j] = in[s] ? ldg_stream(src[s] + at + 4 * j) : make_uint4(0, 0, 0, 0);
+    };
+    // Sixteen terms to an accumulator of their own, these then added in a tree; the terms' magnitudes in a chain beside them.
+    auto multiply = [&](float (&sum)[4], float (&mag)[4], const Half& x, int sign) {
+      float part[2 * NJ][4];
+      auto term = [&](float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+        constexpr uint32_t kAbs = 0x7fff7fffu;
+        d[0] = d[1] = d[2] = d[3] = 0.f;
+        mma_bf16_16816(d, a0, a1, a2, a3, b0, b1);
+        mma_bf16_16816(mag, a0 & kAbs, a1 & kAbs, a2 & kAbs, a3 & kAbs, b0 & kAbs, b1 & kAbs);
+      };
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const uint4 y = sh.q[sign][j][lane];
+        term(part[2 * j], x[0][j].x, x[1][j].x, x[0][j].y, x[1][j].y, y.x, y.y);
+        term(part[2 * j + 1], x[0][j].z, x[1][j].z, x[0][j].w, x[1][j].w, y.z, y.w);
       }
 #pragma unroll
-      for (int off = kLanes / 2; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      qsum = isnan(qsum) || qsum > sum ? qsum : sum;
+      for (int step = 1; step < 2 * NJ; step *= 2)
+#pragma unroll
+        for (int i = 0; i + step < 2 * NJ; i += 2 * step)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) part[i][e] += part[i + step][e];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] = part[0][e];
+    };
+    Half lo, hi;
+    if (run < tiles) {
+      find(0, run);
+      load(lo, 0);
+      load(hi, D / 8);
     }
-    if (tid == 0) sh.qsum = qsum;
-    if (splits > 1) cluster_wait();  // the first CTA runs: its shared memory may be written
-    const uint32_t keys0 = splits > 1 ? cluster_addr(ptx::smem_u32(keys), 0) : 0;
-    uint32_t big = 0;  // largest magnitude among the bounds, two at a time
-    for (int i0 = begin; i0 < end; i0 += kAtOnce * kDeep) {
-      if (i0 - at >= 32) {
-        cur = nxt;
-        at += 32;
-        nxt = table_entry(at + 32 + lane);
+    __syncthreads();  // (the query is in shared memory)
+    for (int tile = run, n = 0; tile < tiles; tile += runs, ++n) {
+      float low[4], high[4], mag[4] = {0.f, 0.f, 0.f, 0.f}, mag2[4] = {0.f, 0.f, 0.f, 0.f};
+      const bool more = tile + runs < tiles;
+      if (more) find(n + 1, tile + runs);
+      multiply(low, mag, lo, 0);
+      if (more) load(lo, 0);
+      multiply(high, mag2, hi, 1);
+      if (more) load(hi, D / 8);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        low[e] += high[e];
+        mag[e] += mag2[e];
       }
-      uint32_t lo[kDeep][kDims / 2], hi[kDeep][kDims / 2];
+      // elements 0, 1: page r, heads 2c and 2c + 1; 2, 3: page r + 8
 #pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        const int pg = __shfl_sync(0xffffffffu, cur, i0 - at + u * kAtOnce + sub);
-        const __nv_bfloat16* src = base + pg * page_stride + dim0;
-        if (i0 + u * kAtOnce + sub < end) {
-          load_dims<kDims>(lo[u], src);
-          load_dims<kDims>(hi[u], src + D);
-        } else {
-#pragma unroll
-          for (int w = 0; w < kDims / 2; ++w) lo[u][w] = hi[u][w] = 0;
+      for (int s = 0; s < 2; ++s) {
+        float best = fmaxf(2 * c < G ? low[2 * s] : -INFINITY, 2 * c + 1 < G ? low[2 * s + 1] : -INFINITY);
+        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
+        const int i = 16 * tile + 8 * s + r;
+        if (i < m) {
+          const uint32_t key = key_of(best);
+          least = min(least, key);
+          most = max(most, key);
+          if (c == s) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys_at + i * 8 + 4), "r"(key) : "memory");
         }
-      }
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        float sum[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) sum[g] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kDims / 2; ++w) {
-          big = __vmaxu2(big, __vmaxu2(lo[u][w] & 0x7fff7fffu, hi[u][w] & 0x7fff7fffu));
-          const float l0 = low_half(lo[u][w]), l1 = high_half(lo[u][w]), h0 = low_half(hi[u][w]), h1 = high_half(hi[u][w]);
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            sum[g] = fmaf(qp[g][2 * w], h0, sum[g]);
-            sum[g] = fmaf(qn[g][2 * w], l0, sum[g]);
-            sum[g] = fmaf(qp[g][2 * w + 1], h1, sum[g]);
-            sum[g] = fmaf(qn[g][2 * w + 1], l1, sum[g]);
-          }
-        }
-        const float best = largest_sum<G, kLanes>(sum);
-        const int i = i0 + u * kAtOnce + sub;
-        if (lane % kLanes == 0 && i < end) {
-          const u64 key = (u64)key_of(best) << 32;
-          if (splits > 1)
-            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(keys0 + i * 8), "l"(key) : "memory");
-          else
-            keys[i] = key;
-        }
+        reach = max(reach, max(__float_as_uint(mag[2 * s]) & 0x7fffffffu, __float_as_uint(mag[2 * s + 1]) & 0x7fffffffu));  // (not a number: above all)
       }
     }
-    big = max(big & 0xffffu, big >> 16);
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, off));
-    if (lane == 0) sh.warp_bmax[warp] = big;
-    __syncthreads();
-    if (tid == 0) {
-#pragma unroll
-      for (int w = 0; w < kSelWarps; ++w) big = max(big, sh.warp_bmax[w]);
-      if (splits > 1)
-        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr(ptx::smem_u32(&sh.bmax[rank]), 0)), "r"(big) : "memory");
-      else
-        sh.bmax[0] = big;
+    reach = __reduce_max_sync(0xffffffffu, reach);
+    least = __reduce_min_sync(0xffffffffu, least);
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0) {
+      const uint32_t lo0 = ptx::smem_u32(&sh.run_lo[run]), hi0 = ptx::smem_u32(&sh.run_hi[run]), reach0 = ptx::smem_u32(&sh.run_reach[run]);
+      const uint32_t shift = keys_at - keys0;  // to the first CTA
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(lo0 + shift), "r"(least) : "memory");
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(hi0 + shift), "r"(most) : "memory");
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(reach0 + shift), "r"(reach) : "memory");
     }
     if (splits > 1) {
       cluster_arrive();
@@ -357,100 +336,143 @@ __global__ void __launch_bounds__(kSelThreads) select_pages_kernel(const SelectA
     cluster_wait();
   }
   ptx::launch_dependents();
-  if (rank != 0) return;
+  if (rank != 0 || !fits) return;
+  if (all) {
+    for (int i = tid; i < a.n_select; i += kThreads) list[i] = i < nb ? i : -1;
+    if (tid == 0) a.counts[row] = nb;
+    return;
+  }
+  for (int i = tid; i < a.n_first; i += kThreads) list[i] = i;
+  for (int i = tid; i < a.n_last; i += kThreads) list[a.n_select - a.n_last + i] = nb - a.n_last + i;
+  if (tid == 0) a.counts[row] = a.n_select;
+  if (!scored) return;
 
   // ---- the choice, by the first CTA
-  Choice ch{~0ull, 0};
-  if (need > 0) {
-    ch = choose(sh, keys, m, need);
-    uint32_t big = 0;
-    for (int s = 0; s < splits; ++s) big = max(big, sh.bmax[s]);
-    // A sum of a lane takes 2 kDims roundings, the sum over the lanes five at most, and so each partial sum of at most (sum |q|) max |bound| is
-    // rounded no more than 21 times, each by 2^-24 of itself: below 2^-19 of it in all.  Twice that for the sum of |q| itself; what is too small
-    // for 32 bits adds less than 2^-140.
-    const float err = sh.qsum * low_half(big) * 0x1p-18f + 0x1p-140f;
-    u64 lo = ~0ull, hi = 0;  // the smallest key chosen, the largest one left
-    int seen_eq = 0;
-    for (int i = tid; i < m; i += kSelThreads) {
-      const u64 k = keys[i];
-      if (surely(ch, k)) lo = min(lo, k);
-      else hi = max(hi, k);
-      seen_eq |= equals(ch, k);
-    }
-    if (__syncthreads_or(seen_eq)) lo = min(lo, ch.ge - 1);  // (equals chosen and, maybe, equals left)
-    block_range(sh, lo, hi);
-    const float kept = value_of((uint32_t)(lo >> 32)), left = value_of((uint32_t)(hi >> 32));
-    if (m > need && !(kept - left > 2.f * err)) {
-      for (int i0 = warp; i0 < m; i0 += kSelWarps) {
-        const float v = value_of((uint32_t)(keys[i0] >> 32));
-        u64 k = v > kept + 2.f * err ? ~0ull : 0ull;
-        if (k == 0 && !(v < kept - 2.f * err)) {
-          int pg = ptx::ld_plain(table + i0);
-          if ((unsigned)pg >= (unsigned)a.pool.num_pages) pg = 0;  // (reported above)
-          k = exact_key<D, G>(q, base + pg * page_stride);
-        }
-        __syncwarp();
-        if (lane == 0) keys[i0] = k;
-      }
-      __syncthreads();
-      ch = choose(sh, keys, m, need);
-    }
+  uint32_t least = 0xffffffffu, most = 0, reach = 0;
+  for (int i = lane; i < runs; i += 32) {
+    least = min(least, sh.run_lo[i]);
+    most = max(most, sh.run_hi[i]);
+    reach = max(reach, sh.run_reach[i]);
   }
-
-  // ---- the list, ascending: a warp takes a run of the keys
-  const int begin = (int)((int64_t)m * warp / kSelWarps), end = (int)((int64_t)m * (warp + 1) / kSelWarps);
-  int ge = 0, eq = 0;
-  if (need > 0) {
-    for (int i0 = begin; i0 < end; i0 += 32) {
-      const bool in = i0 + lane < end;
-      const u64 k = in ? keys[i0 + lane] : 0;
-      ge += __popc(__ballot_sync(0xffffffffu, in && surely(ch, k)));
-      eq += __popc(__ballot_sync(0xffffffffu, in && equals(ch, k)));
-    }
+  least = __reduce_min_sync(0xffffffffu, least);
+  most = __reduce_max_sync(0xffffffffu, most);
+  reach = __reduce_max_sync(0xffffffffu, reach);
+  int turn = 0;
+  Choice ch = choose<uint32_t>(sh, keys, m, need, least, most, turn);
+  // Of what the terms' magnitudes add up to, an accumulator loses 2^-23 with each of its sixteen terms at most, the tree 2^-24 with each of its four
+  // steps: below 2^-18.8 in all; their sum as computed, by accumulators of 128 terms, is short by 2^-16 of itself at most.  Elements of the bounds below
+  // the normal numbers may count as 0 (2^-126 |q_d| each), as may sums.
+  float qsum = 0.f;  // at least the sum of |q_d| of any head
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) qsum += sh.qsum[j];
+  const float err = __uint_as_float(reach) * 0x1p-18f + qsum * 0x1p-125f + 0x1p-120f;
+  // marks: of each 32 keys, those surely chosen and those that are equal to the last one chosen
+  const int groups = (m + 31) / 32;
+  uint2* marks = reinterpret_cast<uint2*>(keys + a.bound_pages);
+  uint32_t kept = 0xffffffffu, left = 0;  // the smallest key chosen, the largest one left
+  for (int g = warp; g < groups; g += kWarps) {
+    const int i = 32 * g + lane;
+    const uint32_t k = i < m ? key_at<uint32_t>(keys, i) : 0;
+    const bool in = i < m && surely(ch, k), eq = i < m && equals(ch, k);
+    const unsigned ins = __ballot_sync(0xffffffffu, in), eqs = __ballot_sync(0xffffffffu, eq);
+    if (in || eq) kept = min(kept, k);
+    if (i < m && !in) left = max(left, k);  // (of equals, some are chosen and some are left)
+    if (lane == 0) marks[g] = make_uint2(ins, eqs);
   }
+  kept = __reduce_min_sync(0xffffffffu, kept);
+  left = __reduce_max_sync(0xffffffffu, left);
   if (lane == 0) {
-    sh.warp_ge[warp] = ge;
-    sh.warp_eq[warp] = eq;
+    sh.warp_kept[warp] = kept;
+    sh.warp_left[warp] = left;
   }
   __syncthreads();
-  int out = a.n_first, eq_left = ch.eq;
-  for (int w = 0; w < warp; ++w) {
-    out += sh.warp_ge[w] + min(eq_left, sh.warp_eq[w]);
-    eq_left -= min(eq_left, sh.warp_eq[w]);
-  }
-  if (need > 0) {
-    for (int i0 = begin; i0 < end; i0 += 32) {
-      const bool in = i0 + lane < end;
-      const u64 k = in ? keys[i0 + lane] : 0;
-      const unsigned eqs = __ballot_sync(0xffffffffu, in && equals(ch, k));
-      const bool take = in && (surely(ch, k) || (equals(ch, k) && __popc(eqs & ((1u << lane) - 1)) < eq_left));
-      const unsigned takes = __ballot_sync(0xffffffffu, take);
-      if (take) list[out + __popc(takes & ((1u << lane) - 1))] = a.n_first + i0 + lane;
-      out += __popc(takes);
-      eq_left -= min(eq_left, __popc(eqs));
+  kept = __reduce_min_sync(0xffffffffu, lane < kWarps ? sh.warp_kept[lane] : 0xffffffffu);
+  left = __reduce_max_sync(0xffffffffu, lane < kWarps ? sh.warp_left[lane] : 0);
+  const float low = value_of(kept), next = value_of(left);
+  if (!(low - next > 2.f * err)) {
+    u64 lo = kAbove, hi = kBelow;
+    int above = 0, rest = need;
+    for (int g = warp; g < groups; g += kWarps) {
+      const int i = 32 * g + lane;
+      const float v = i < m ? value_of(key_at<uint32_t>(keys, i)) : 0.f;
+      const bool over = i < m && v > low + 2.f * err, near = i < m && !over && !(v < low - 2.f * err);
+      u64 mine = over ? kAbove : kBelow;
+      above += __popc(__ballot_sync(0xffffffffu, over));
+      for (unsigned open = __ballot_sync(0xffffffffu, near); open != 0; open &= open - 1) {
+        const int at = __ffs(open) - 1;
+        int pg = ptx::ld_plain(table + 32 * g + at);
+        if ((unsigned)pg >= (unsigned)a.pool.num_pages) pg = 0;  // (reported above)
+        const u64 k = exact_key<D>(q, base + pg * page_stride, G);
+        if (lane == at) mine = k;
+        lo = min(lo, k);
+        hi = max(hi, k);
+      }
+      if (i < m) keys[i] = mine;
     }
+    if (lane == 0) {
+      sh.warp_lo[warp] = lo;
+      sh.warp_hi[warp] = hi;
+      sh.warp_above[warp] = above;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      lo = min(lo, sh.warp_lo[w]);
+      hi = max(hi, sh.warp_hi[w]);
+      rest -= sh.warp_above[w];
+    }
+    ch = choose<u64>(sh, keys, m, rest, lo, hi, turn);
+    for (int g = warp; g < groups; g += kWarps) {
+      const int i = 32 * g + lane;
+      const u64 k = i < m ? keys[i] : 0;
+      const unsigned ins = __ballot_sync(0xffffffffu, i < m && surely(ch, k)), eqs = __ballot_sync(0xffffffffu, i < m && equals(ch, k));
+      if (lane == 0) marks[g] = make_uint2(ins, eqs);
+    }
+    __syncthreads();
   }
-  for (int i = tid; i < a.n_first; i += kSelThreads) list[i] = i;
-  for (int i = tid; i < a.n_last; i += kSelThreads) list[a.n_select - a.n_last + i] = nb - a.n_last + i;
-  if (tid == 0) a.counts[row] = a.n_select;
+
+  // ---- the list, ascending: every warp counts all the marks, 32 groups at a time, and writes the groups that are its own
+  int out = a.n_first, eq_before = 0;
+  for (int g0 = 0; g0 < groups; g0 += 32) {
+    const uint2 mark = g0 + lane < groups ? marks[g0 + lane] : make_uint2(0, 0);
+    int n_in = __popc(mark.x), n_eq = __popc(mark.y);
+    const int own_in = n_in, own_eq = n_eq;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, n_in, off), y = __shfl_up_sync(0xffffffffu, n_eq, off);
+      if (lane >= off) {
+        n_in += x;
+        n_eq += y;
+      }
+    }
+    const int all_in = __shfl_sync(0xffffffffu, n_in, 31), all_eq = __shfl_sync(0xffffffffu, n_eq, 31);
+    const int eqs_at = eq_before + n_eq - own_eq;                                       // equals in front of the group
+    const int at = out + n_in - own_in + min(ch.eq, eqs_at) - min(ch.eq, eq_before);    // its first place in the list
+    for (int g = (warp - g0 % kWarps + kWarps) % kWarps; g < 32 && g0 + g < groups; g += kWarps) {
+      const unsigned ins = __shfl_sync(0xffffffffu, mark.x, g), eqs = __shfl_sync(0xffffffffu, mark.y, g);
+      const int first = __shfl_sync(0xffffffffu, at, g), room = ch.eq - __shfl_sync(0xffffffffu, eqs_at, g);
+      const unsigned below = (1u << lane) - 1;
+      const bool take = (ins >> lane & 1) || ((eqs >> lane & 1) && __popc(eqs & below) < room);
+      const unsigned takes = __ballot_sync(0xffffffffu, take);
+      if (take) list[first + __popc(takes & below)] = a.n_first + 32 * (g0 + g) + lane;
+    }
+    out += all_in + min(ch.eq, eq_before + all_eq) - min(ch.eq, eq_before);
+    eq_before += all_eq;
+  }
 }
 
-template <int D, int G>
-static kv_status_t launch_select_variant(const kv_pool_t* p, const SelectArgs& a, int rows, cudaStream_t st) {
+// Shared memory for the keys of so many pages and for the marks.
+static int select_smem(int pages) { return pages * 8 + (pages + 31) / 32 * 8; }
+
+template <int D, int kWarps>
+static kv_status_t launch_select(const kv_pool_t* p, const SelectArgs& a, int rows, cudaStream_t st) {
   static std::atomic<bool> ready[kMaxDevices];
-  const auto prepare = [] {
-    return cudaFuncSetAttribute(select_pages_kernel<D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelMaxPages * 8) == cudaSuccess &&
-           cudaFuncSetAttribute(select_pages_kernel<D, G>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
-  };
-  if (!once_per_device(ready, p->device, prepare)) {
-    cudaGetLastError();
-    return KV_ERR_CUDA;
-  }
+  if (!allow_smem((const void*)select_pages_kernel<D, kWarps>, select_smem(kSelMaxPages), ready, p->device)) return KV_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
   cfg.gridDim = dim3((unsigned)(rows * a.splits));
-  cfg.blockDim = dim3(kSelThreads);
-  cfg.dynamicSmemBytes = (size_t)a.bound_pages * 8;
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = (size_t)select_smem(a.bound_pages);
   cfg.stream = st;
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -459,19 +481,9 @@ static kv_status_t launch_select_variant(const kv_pool_t* p, const SelectArgs& a
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.splits > 1 ? 2 : 1;
-  KV_CUDA_OK(cudaLaunchKernelEx(&cfg, select_pages_kernel<D, G>, a));
+  KV_CUDA_OK(cudaLaunchKernelEx(&cfg, select_pages_kernel<D, kWarps>, a));
   count_launch();
   return KV_OK;
-}
-
-template <int D>
-static kv_status_t launch_select(const kv_pool_t* p, const SelectArgs& a, int rows, int group, cudaStream_t st) {
-  switch (group) {
-    case 1: return launch_select_variant<D, 1>(p, a, rows, st);
-    case 2: return launch_select_variant<D, 2>(p, a, rows, st);
-    case 4: return launch_select_variant<D, 4>(p, a, rows, st);
-    default: return launch_select_variant<D, 8>(p, a, rows, st);
-  }
 }
 
 }  // namespace kvattn
@@ -494,10 +506,28 @@ extern "C" kv_status_t attn_select_pages(kv_pool_t* p, const void* q, int n_q_he
   const int64_t rows = (int64_t)batch * p->n_kv_heads, bound = ((int64_t)max_ctx_len + kPageSize - 1) / kPageSize;
   if (bound > kSelMaxPages || rows * kSelMaxSplits > 0x7fffffffLL) return KV_ERR_UNSUPPORTED;
   SelectArgs a{p->view(), (const __nv_bfloat16*)q, (const __nv_bfloat16*)bounds, block_tables, ctx_lens, pages, counts, max_pages, (int)bound,
-               n_q_heads, n_select, n_first, n_last, 1};
-  // As many CTAs to a row as the device has room for beside the other rows, while a warp still has sixteen pages.
+               group, n_select, n_first, n_last, 1};
+  // CTAs of eight warps, two of them to an SM, or of four, four to an SM, and as many to a row as the device holds and find sixteen pages for most of
+  // their warps: whatever leaves the SM with most to read the least (an SM reads 64 GB/s at best).  Us with eight warps and 1 / 2 / 4 / 8 CTAs, four warps and
+  // 1 / 2 / 4 (heads of 128, 8 to a group): 8 rows of 722 pages 12.0 / 9.1 / 7.9 / 6.7, 16.1 / 11.1 / 8.3; 64 rows of 512-1024 19.8 / 16.8 / 14.6 / 17.8,
+  // 27.0 / 19.9 / 16.2; 240 of 63-94 7.7 / 12.6 / - / -, 8.0 / 8.1 / 11.7; 256 of 512-1024 28.4 / 33.1 / - / -, 35.5 / 29.4 / 30.8; 2048 of 64-256 56.0
+  // and 41.7 with one.  Few rows that are longer still: sixteen warps, 8 rows of 6250 pages, heads of 64, 15.6 / 13.1 with eight / sixteen.
   const int sms = sm_count_of(p->device);
-  while (a.splits < kSelMaxSplits && rows * a.splits * 2 <= 2 * sms && bound >= (int64_t)a.splits * 2 * kSelWarps * 16) a.splits *= 2;
-  return p->head_dim == 128 ? launch_select<128>(p, a, (int)rows, group, (cudaStream_t)stream)
-                            : launch_select<64>(p, a, (int)rows, group, (cudaStream_t)stream);
+  const int64_t tiles = (bound + 15) / 16, resident = 16 * (int64_t)sms;  // (warps)
+  int warps = 4;
+  double least = 1e30;
+  for (int w : {8, 4})
+    for (int s = 1; s <= kSelMaxSplits && (s == 1 || (rows * s * w <= resident && 2 * tiles > (int64_t)s * w)); ++s) {
+      const double most = (double)((rows * s + sms - 1) / sms) / s;
+      if ((w == 8 && rows * w > resident) || most > (w == 8 ? least : 0.9 * least)) continue;
+      least = most;
+      warps = w;
+      a.splits = s;
+    }
+  if (a.splits == kSelMaxSplits && rows * 16 * a.splits <= resident && tiles > 4 * a.splits * warps) warps = 16;
+  const auto go = [&](auto w) {
+    return p->head_dim == 128 ? launch_select<128, decltype(w)::value>(p, a, (int)rows, (cudaStream_t)stream)
+                              : launch_select<64, decltype(w)::value>(p, a, (int)rows, (cudaStream_t)stream);
+  };
+  return warps == 16 ? go(std::integral_constant<int, 16>()) : warps == 8 ? go(std::integral_constant<int, 8>()) : go(std::integral_constant<int, 4>());
 }
