@@ -309,7 +309,7 @@ kv_status_t attn_mixed(kv_pool_t* pool, int n_q_heads, float scale, const attn_e
  * next_lens[i] = ctx_lens[i] + new_lens[i] [dev][batch] (NULL: not wanted), *next_cursor = *cursor + pages taken (NULL: not wanted).
  * next_lens may be ctx_lens and next_cursor may be cursor (a step that is captured once and replayed); no other overlap.
  * A sequence gets nothing - no page, slots -1, position 0, next_lens = ctx_lens - and KV_ERR_BOUNDS is recorded, if a length is
- * negative, its tokens go beyond max_pages pages or its rows beyond total_new, or new_pages has run out (then no later sequence gets
+ * negative, its tokens go beyond max_pages pages or 2^31 - 1, or its rows beyond total_new, or new_pages has run out (then no later sequence gets
  * a page either).  A page id outside the pool gives its rows slot -1 and records KV_ERR_BOUNDS.  KV_ERR_UNSUPPORTED: total_new or
  * n_new_pages above 2^30. */
 kv_status_t kv_step_tables(kv_pool_t* pool, const int* ctx_lens, const int* new_lens, int batch, const int* new_pages, int n_new_pages,
@@ -337,7 +337,8 @@ kv_status_t kv_append_rotary(kv_pool_t* pool, const void* q, int64_t q_stride, c
 /* Bounds of the keys of every page that rows have been stored in: bounds [dev] bf16 [num_pages][n_kv_heads][2][head_dim],
  * kv_page_bounds_bytes() bytes, 16-byte aligned, the caller's; [..][0][d] is the smallest and [..][1][d] the largest k_d among the page's
  * tokens (0 .. the slot of its last row in this call).  slots [dev][total_new] as the rows were stored with; the pages hold these keys
- * already.  Bounds of other pages stay.  A key element that is not a number makes both bounds of its dim not a number. */
+ * already.  Bounds of other pages stay.  A key element that is not a number makes both bounds of its dim not a number.  A slot outside the
+ * pool is passed over and recorded as KV_ERR_BOUNDS.  KV_ERR_UNSUPPORTED: total_new above 2^30. */
 size_t kv_page_bounds_bytes(const kv_pool_t* pool);
 kv_status_t kv_page_bounds(kv_pool_t* pool, const int* slots, int total_new, void* bounds, void* stream);
 
@@ -350,6 +351,7 @@ kv_status_t kv_page_bounds(kv_pool_t* pool, const int* slots, int total_new, voi
  * [n_select] receives the pages as blocks of the sequence (indices into its block-table row), ascending, then -1; counts [dev][batch]
  * [n_kv_heads] how many.  ctx_lens[i] <= 0: none.  max_ctx_len: host upper bound; a longer sequence is recorded as KV_ERR_BOUNDS and its
  * rows are left unwritten, and so is a block-table entry outside the pool (its row's pages are then not to be trusted).
+ * Table entries past the context may be read and are not used.
  * KV_ERR_INVALID: n_first + n_last > n_select.  KV_ERR_UNSUPPORTED: max_ctx_len above 24576 pages. */
 kv_status_t attn_select_pages(kv_pool_t* pool, const void* q, int n_q_heads, const void* bounds, const int* block_tables, int max_pages,
                               const int* ctx_lens, int batch, int max_ctx_len, int n_select, int n_first, int n_last, int* pages,

@@ -124,7 +124,7 @@ size_t kv_page_bounds_bytes(const kv_pool_t* p) {
 
 kv_status_t kv_page_bounds(kv_pool_t* p, const int* slots, int total_new, void* bounds, void* stream) {
   if (p == nullptr || total_new < 0) return KV_ERR_INVALID;
-  if (p->num_pages > (1 << 27)) return KV_ERR_UNSUPPORTED;
+  if (p->num_pages > (1 << 27) || total_new > (1 << 30)) return KV_ERR_UNSUPPORTED;
   if (total_new == 0) return KV_OK;
   if (slots == nullptr || bounds == nullptr || (((uintptr_t)bounds) & 15) != 0) return KV_ERR_INVALID;
   if (!on_pool_device(p)) return KV_ERR_INVALID;

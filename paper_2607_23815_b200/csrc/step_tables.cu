@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(kTableThreads) step_tables_kernel(const Tables
   const int cursor = a.cursor != nullptr ? ptx::ld_plain(a.cursor) : 0;
   const bool cursor_ok = cursor >= 0 && cursor <= a.n_new_pages;
   const unsigned avail = cursor_ok ? a.n_new_pages - cursor : 0;
+  const int64_t room = min((int64_t)a.max_pages * kPageSize, (int64_t)0x7fffffff);  // tokens of a sequence: a row of its table, and a length has 31 bits
   const bool speaks = blockIdx.x == 0;  // one block writes what belongs to the sequences, and reports
   bool bad = !cursor_ok;
   if (tid == 0) taken = 0;
@@ -79,7 +80,7 @@ __global__ void __launch_bounds__(kTableThreads) step_tables_kernel(const Tables
     const unsigned n_rows = n > 0 ? min((unsigned)n, kSumLimit) : 0;
     unsigned all_rows, all_pages;
     const unsigned row = add_limited(rows, block_sum(n_rows, warp_sums, &all_rows)), row_end = add_limited(row, n_rows);
-    bool ok = c >= 0 && n >= 0 && (int64_t)c + n <= (int64_t)a.max_pages * kPageSize && row_end <= (unsigned)a.total_new;
+    bool ok = c >= 0 && n >= 0 && (int64_t)c + n <= room && row_end <= (unsigned)a.total_new;
     const int have = ok ? (int)(((int64_t)c + kPageSize - 1) / kPageSize) : 0;
     const unsigned need = ok ? (unsigned)(((int64_t)c + n + kPageSize - 1) / kPageSize) - have : 0;
     const unsigned page = add_limited(pages, block_sum(need, warp_sums, &all_pages)), page_end = add_limited(page, need);

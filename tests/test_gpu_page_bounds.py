@@ -67,7 +67,8 @@ def test_slots_outside_are_recorded_and_nothing_to_do():
     call = kvattn.lib().kv_page_bounds
     h, inv = pages.pool.handle, kvattn.KV_ERR_INVALID
     assert call(None, p(), 1, p(), None) == call(h, None, 1, p(), None) == call(h, p(), 1, None, None) == call(h, p(), -1, p(), None) == inv
-    assert call(h, p(), 1, p(8), None) == inv and kvattn.kvattn_launch_count() == n0
+    assert call(h, p(), 1, p(8), None) == inv and call(h, p(), (1 << 30) + 1, p(), None) == kvattn.KV_ERR_UNSUPPORTED
+    assert kvattn.kvattn_launch_count() == n0
     assert kvattn.kv_page_bounds_bytes(pages.pool) == 2 * 2 * 64 * 2 and kvattn.lib().kv_page_bounds_bytes(None) == 0
     with pytest.raises(ValueError):
         kvattn.kv_page_bounds(pages.pool, i32([1]), b[:1])

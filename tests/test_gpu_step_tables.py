@@ -108,6 +108,19 @@ def test_what_does_not_fit_gets_nothing_and_is_recorded(what, n, in_place):
     assert pages.status() == kvattn.KV_ERR_BOUNDS and pages.status() == 0
 
 
+def test_a_length_has_31_bits():
+    width = (1 << 27) + 2
+    pages, bt = Pages(4, 1, 64), torch.empty((1, width), dtype=torch.int32, device="cuda")
+    bt[0, -3:] = 1
+    for ctx, new, ok in ((0x7ffffffe, 1, True), (0x7ffffffe, 2, False), (0x7fffffff, 0, True), (0x7ffffff0, 0x7fffffff, False)):
+        total = min(new, 40)
+        cu, pos, slots, nxt, cur = i32([0, 0]), i32([9] * total), i32([9] * total), i32([5]), i32([0])
+        kvattn.kv_step_tables(pages.pool, i32([ctx]), i32([new]), i32([2]), bt, cu, pos, slots, nxt, None, cur)
+        assert int(nxt) == ctx + (new if ok else 0) and int(cur) == 0
+        assert slots.tolist() == ([16 + 14] * total if ok else [-1] * total) and pos.tolist() == ([ctx] * total if ok else [0] * total)
+        assert pages.status() == (0 if ok else kvattn.KV_ERR_BOUNDS)
+
+
 def test_no_sequences_and_no_positions():
     pages = Pages(4, 1, 64)
     got = _run(pages, [], [], [1, 2], np.zeros((0, 3)), 5)
