@@ -11,7 +11,11 @@
 // What bounds it: HBM (4 D bytes a page and KV head, read once) where there are many rows, latency where there are few, so a row's pages are then
 // shared out over a cluster whose CTAs push their scores into the shared memory of the first, which chooses.  A score is a product of (q+, q-), the
 // positive and the negative part of q, with (hi, lo): sixteen pages by eight heads in an mma.sync.m16n8k16 whose A fragments are the 16-byte chunks as
-// they lie.
+// they lie.  (The lanes' own multiplications, G for every element, and their sums by shuffles took 103 us where this takes 27.5; the tensor
+// pipe is busy a tenth of the time.)  32 documents of 8192-16384 tokens, 64/8 heads of 128: 27.5 us, 3.6 TB/s; 15 us of it are the bytes, the rest is what a
+// row has in front of them (length, page ids, the first pages: three trips to memory) and behind them (the choice, 2 to 3 us), at which no other row's
+// pages are read: the rows are on the device all at once.  256 sequences of 1024-4096: 43 us, 3.9 TB/s.  One of 15000: 5.7 us.  What has been left:
+// rows of the next round fetched in front of the choice, which only batches of more than four rows to an SM would gain by.
 #include <math.h>
 
 #include <type_traits>
@@ -61,7 +65,7 @@ __device__ __forceinline__ Key key_at(const u64* keys, int i) {
 }
 
 struct SelectShared {
-  uint4 q[2][4][32];  // [negative, positive elements][16-byte chunk 4 j + c of head r, by j][lane (r, c)]
+  uint4 q[3][4][32];  // [negative elements, positive ones, all without their signs][16-byte chunk 4 j + c of head r, by j][lane (r, c)]
   float qsum[kSelMaxWarps];
   unsigned hist[3][kBins];
   // of each run of pages: the smallest and the largest key, the largest sum of magnitudes of a score's terms (bits)
@@ -130,6 +134,12 @@ __device__ __forceinline__ Choice choose(SelectShared& sh, const u64* keys, int 
   return Choice{(u64)lo + 1, need};  // all that is left is equal
 }
 
+// The larger of the magnitudes of two pairs of bf16 (not a number, if one of them is not).
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hmax2_nan(__habs2(*reinterpret_cast<const __nv_bfloat162*>(&a)), __habs2(*reinterpret_cast<const __nv_bfloat162*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
 // The score by its definition, in 64 bits, for the whole warp.
 template <int D>
 __device__ __forceinline__ u64 exact_key(const __nv_bfloat16* q, const __nv_bfloat16* bounds, int group) {
@@ -192,6 +202,8 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
   if (warp < NJ) {  // head r's chunks 4 warp + c: the positive elements (for hi) and the others (for lo)
     const uint4 x = r < G ? ptx::ld_plain(reinterpret_cast<const uint4*>(q + r * D) + 4 * warp + c) : make_uint4(0, 0, 0, 0);
     uint4 pos, neg;
+    constexpr uint32_t kAbs = 0x7fff7fffu;  // two elements without their signs
+    const uint4 any = make_uint4(x.x & kAbs, x.y & kAbs, x.z & kAbs, x.w & kAbs);
     float sum = 0.f;
     bool odd = false;  // an element below the normal numbers, which the tensor cores may take for 0
     auto split = [&](uint32_t w, uint32_t& pos, uint32_t& neg) {
@@ -207,6 +219,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
     split(x.w, pos.w, neg.w);
     sh.q[0][warp][lane] = neg;
     sh.q[1][warp][lane] = pos;
+    sh.q[2][warp][lane] = any;
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     sum = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(sum)));  // (not a number: above all)
@@ -229,8 +242,8 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
     const uint32_t keys0 = ptx::smem_u32(keys), keys_at = splits > 1 ? cluster_addr(keys0, 0) : keys0;
     uint32_t reach = 0, least = 0xffffffffu, most = 0;  // reach: the largest sum of the magnitudes of a score's terms (bits)
     const int tiles = (m + 15) / 16;
-    // A tile's two pages of this lane.  While one half of a tile (lo, then hi) is multiplied, the other one and the same half of the next tile are on
-    // their way.
+    // A tile's two pages of this lane.  A part of a tile that has been multiplied is followed by the same part of the next tile, so that loads are under way
+    // all the time.
     const uint4* src[2];
     bool in[2];
     auto find = [&](int n, int tile) {  // the n-th tile of the warp, each once and in order
@@ -249,61 +262,51 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
         src[s] = reinterpret_cast<const uint4*>(base + pg * page_stride) + c;
       }
     };
-    typedef uint4 Half[2][NJ];
-    auto load = [&](Half& x, int at) {
+    uint4 lo[NJ][2], hi[NJ][2];
+    auto load = [&](int j) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) x[s][j] = in[s] ? ldg_stream(src[s] + at + 4 * j) : make_uint4(0, 0, 0, 0);
-    };
-    // Sixteen terms to an accumulator of their own, these then added in a tree; the terms' magnitudes in a chain beside them.
-    auto multiply = [&](float (&sum)[4], float (&mag)[4], const Half& x, int sign) {
-      float part[2 * NJ][4];
-      auto term = [&](float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-        constexpr uint32_t kAbs = 0x7fff7fffu;
-        d[0] = d[1] = d[2] = d[3] = 0.f;
-        mma_bf16_16816(d, a0, a1, a2, a3, b0, b1);
-        mma_bf16_16816(mag, a0 & kAbs, a1 & kAbs, a2 & kAbs, a3 & kAbs, b0 & kAbs, b1 & kAbs);
-      };
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const uint4 y = sh.q[sign][j][lane];
-        term(part[2 * j], x[0][j].x, x[1][j].x, x[0][j].y, x[1][j].y, y.x, y.y);
-        term(part[2 * j + 1], x[0][j].z, x[1][j].z, x[0][j].w, x[1][j].w, y.z, y.w);
+      for (int s = 0; s < 2; ++s) {
+        lo[j][s] = in[s] ? ldg_stream(src[s] + 4 * j) : make_uint4(0, 0, 0, 0);
+        hi[j][s] = in[s] ? ldg_stream(src[s] + D / 8 + 4 * j) : make_uint4(0, 0, 0, 0);
       }
-#pragma unroll
-      for (int step = 1; step < 2 * NJ; step *= 2)
-#pragma unroll
-        for (int i = 0; i + step < 2 * NJ; i += 2 * step)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) part[i][e] += part[i + step][e];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] = part[0][e];
     };
-    Half lo, hi;
     if (run < tiles) {
       find(0, run);
-      load(lo, 0);
-      load(hi, D / 8);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) load(j);
     }
     __syncthreads();  // (the query is in shared memory)
     for (int tile = run, n = 0; tile < tiles; tile += runs, ++n) {
-      float low[4], high[4], mag[4] = {0.f, 0.f, 0.f, 0.f}, mag2[4] = {0.f, 0.f, 0.f, 0.f};
       const bool more = tile + runs < tiles;
       if (more) find(n + 1, tile + runs);
-      multiply(low, mag, lo, 0);
-      if (more) load(lo, 0);
-      multiply(high, mag2, hi, 1);
-      if (more) load(hi, D / 8);
+      // Sixteen terms to an accumulator of their own, these then added in a tree; the magnitudes of the terms, or more, in a chain beside them.
+      float sum[NJ][4], mag[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        low[e] += high[e];
-        mag[e] += mag2[e];
+      for (int j = 0; j < NJ; ++j) {
+        const uint4 neg = sh.q[0][j][lane], pos = sh.q[1][j][lane], any = sh.q[2][j][lane];
+        float part[4][4];
+        mma_bf16_16816_first(part[0], lo[j][0].x, lo[j][1].x, lo[j][0].y, lo[j][1].y, neg.x, neg.y);
+        mma_bf16_16816_first(part[1], lo[j][0].z, lo[j][1].z, lo[j][0].w, lo[j][1].w, neg.z, neg.w);
+        mma_bf16_16816_first(part[2], hi[j][0].x, hi[j][1].x, hi[j][0].y, hi[j][1].y, pos.x, pos.y);
+        mma_bf16_16816_first(part[3], hi[j][0].z, hi[j][1].z, hi[j][0].w, hi[j][1].w, pos.z, pos.w);
+        mma_bf16_16816(mag, larger(lo[j][0].x, hi[j][0].x), larger(lo[j][1].x, hi[j][1].x), larger(lo[j][0].y, hi[j][0].y), larger(lo[j][1].y, hi[j][1].y),
+                       any.x, any.y);
+        mma_bf16_16816(mag, larger(lo[j][0].z, hi[j][0].z), larger(lo[j][1].z, hi[j][1].z), larger(lo[j][0].w, hi[j][0].w), larger(lo[j][1].w, hi[j][1].w),
+                       any.z, any.w);
+        if (more) load(j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[j][e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
       }
+#pragma unroll
+      for (int step = 1; step < NJ; step *= 2)
+#pragma unroll
+        for (int j = 0; j + step < NJ; j += 2 * step)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[j][e] += sum[j + step][e];
       // elements 0, 1: page r, heads 2c and 2c + 1; 2, 3: page r + 8
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        float best = fmaxf(2 * c < G ? low[2 * s] : -INFINITY, 2 * c + 1 < G ? low[2 * s + 1] : -INFINITY);
+        float best = fmaxf(2 * c < G ? sum[0][2 * s] : -INFINITY, 2 * c + 1 < G ? sum[0][2 * s + 1] : -INFINITY);
         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
         const int i = 16 * tile + 8 * s + r;
@@ -360,7 +363,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
   int turn = 0;
   Choice ch = choose<uint32_t>(sh, keys, m, need, least, most, turn);
   // Of what the terms' magnitudes add up to, an accumulator loses 2^-23 with each of its sixteen terms at most, the tree 2^-24 with each of its four
-  // steps: below 2^-18.8 in all; their sum as computed, by accumulators of 128 terms, is short by 2^-16 of itself at most.  Elements of the bounds below
+  // steps: below 2^-18.8 in all; their sum as computed, by an accumulator of 128 terms, is short by 2^-16 of itself at most.  Elements of the bounds below
   // the normal numbers may count as 0 (2^-126 |q_d| each), as may sums.
   float qsum = 0.f;  // at least the sum of |q_d| of any head
 #pragma unroll
