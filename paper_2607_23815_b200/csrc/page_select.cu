@@ -11,10 +11,10 @@
 // What bounds it: HBM (4 D bytes a page and KV head, read once) where there are many rows, latency where there are few, so a row's pages are then
 // shared out over a cluster whose CTAs push their scores into the shared memory of the first, which chooses.  A score is a product of (q+, q-), the
 // positive and the negative part of q, with (hi, lo): sixteen pages by eight heads in an mma.sync.m16n8k16 whose A fragments are the 16-byte chunks as
-// they lie.  (The lanes' own multiplications, G for every element, and their sums by shuffles took 103 us where this takes 27.5; the tensor
-// pipe is busy a tenth of the time.)  32 documents of 8192-16384 tokens, 64/8 heads of 128: 27.5 us, 3.6 TB/s; 15 us of it are the bytes, the rest is what a
+// they lie.  (The lanes' own multiplications, G for every element, and their sums by shuffles took 103 us where this takes 26; the tensor
+// pipe is busy a tenth of the time.)  32 documents of 8192-16384 tokens, 64/8 heads of 128: 26.2 us, 3.8 TB/s; 15 us of it are the bytes, the rest is what a
 // row has in front of them (length, page ids, the first pages: three trips to memory) and behind them (the choice, 2 to 3 us), at which no other row's
-// pages are read: the rows are on the device all at once.  256 sequences of 1024-4096: 43 us, 3.9 TB/s.  One of 15000: 5.7 us.  What has been left:
+// pages are read: the rows are on the device all at once.  256 sequences of 1024-4096: 42 us, 4.1 TB/s.  One of 15000: 5.7 us.  What has been left:
 // rows of the next round fetched in front of the choice, which only batches of more than four rows to an SM would gain by.
 #include <math.h>
 
@@ -43,6 +43,7 @@ constexpr int kSelMaxSplits = 8;
 constexpr int kSelMaxWarps = 16;
 constexpr int kSelMaxPages = 24576;  // 198 KB of keys and marks
 constexpr int kBins = 256;
+constexpr int kNear = 32;
 typedef unsigned long long u64;
 
 // Keys in the order of the values, whatever is not a number above all of them; -0 and 0 are the same.  A page has room for 64 bits in shared memory:
@@ -73,6 +74,9 @@ struct SelectShared {
   uint32_t warp_kept[kSelMaxWarps], warp_left[kSelMaxWarps];
   u64 warp_lo[kSelMaxWarps], warp_hi[kSelMaxWarps];
   int warp_above[kSelMaxWarps];
+  // the first of the pages near the border
+  int near_count, near_page[kNear];
+  u64 near_key[kNear];
 };
 
 // The chosen of the keys are those >= ge and the first `eq` of those that equal ge - 1.
@@ -156,20 +160,26 @@ __device__ __forceinline__ u64 exact_key(const __nv_bfloat16* q, const __nv_bflo
 #pragma unroll
   for (int g = 0; g < 8; ++g)
     if (g < group) load(q + g * D, x[g]);
-  double best = -INFINITY;
+  double sum[8];
 #pragma unroll
   for (int g = 0; g < 8; ++g) {
-    if (g >= group) break;
-    double sum = 0.0;
+    sum[g] = 0.0;
+    if (g < group) {
 #pragma unroll
-    for (int i = 0; i < kDims; ++i) {
-      const double v = value(x[g], i);
-      sum += v * (v >= 0.0 ? value(hi, i) : value(lo, i));
+      for (int i = 0; i < kDims; ++i) {
+        const double v = value(x[g], i);
+        sum[g] += v * (v >= 0.0 ? value(hi, i) : value(lo, i));
+      }
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    best = isnan(best) || best > sum ? best : sum;
   }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+    for (int g = 0; g < 8; ++g) sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], off);
+  double best = sum[0];
+#pragma unroll
+  for (int g = 1; g < 8; ++g)
+    if (g < group) best = isnan(best) || best > sum[g] ? best : sum[g];
   return key_of(best);
 }
 
@@ -184,6 +194,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
   const int Hkv = a.pool.n_kv_heads, G = a.group, seq = row / Hkv, kvh = row - seq * Hkv;
   const int runs = kWarps * splits, run = rank * kWarps + warp;
   for (int b = tid; b < kBins; b += kThreads) sh.hist[0][b] = 0;
+  if (tid == 0) sh.near_count = 0;
   if (splits > 1) cluster_arrive();
   ptx::dependency_wait();
 
@@ -393,43 +404,78 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
   left = __reduce_max_sync(0xffffffffu, lane < kWarps ? sh.warp_left[lane] : 0);
   const float low = value_of(kept), next = value_of(left);
   if (!(low - next > 2.f * err)) {
-    u64 lo = kAbove, hi = kBelow;
+    // Those above the band around the border are chosen, those in it scored again: a few, to each warp its share, of which every lane then sees whether
+    // its own is among the best; or, where there are more, all of them where they are.
     int above = 0, rest = need;
     for (int g = warp; g < groups; g += kWarps) {
       const int i = 32 * g + lane;
       const float v = i < m ? value_of(key_at<uint32_t>(keys, i)) : 0.f;
       const bool over = i < m && v > low + 2.f * err, near = i < m && !over && !(v < low - 2.f * err);
-      u64 mine = over ? kAbove : kBelow;
-      above += __popc(__ballot_sync(0xffffffffu, over));
-      for (unsigned open = __ballot_sync(0xffffffffu, near); open != 0; open &= open - 1) {
-        const int at = __ffs(open) - 1;
-        int pg = ptx::ld_plain(table + 32 * g + at);
-        if ((unsigned)pg >= (unsigned)a.pool.num_pages) pg = 0;  // (reported above)
-        const u64 k = exact_key<D>(q, base + pg * page_stride, G);
-        if (lane == at) mine = k;
-        lo = min(lo, k);
-        hi = max(hi, k);
+      const unsigned overs = __ballot_sync(0xffffffffu, over);
+      above += __popc(overs);
+      if (lane == 0) marks[g] = make_uint2(overs, 0);
+      if (near) {
+        const int at = atomicAdd(&sh.near_count, 1);
+        if (at < kNear) sh.near_page[at] = i;
       }
-      if (i < m) keys[i] = mine;
     }
-    if (lane == 0) {
-      sh.warp_lo[warp] = lo;
-      sh.warp_hi[warp] = hi;
-      sh.warp_above[warp] = above;
-    }
+    if (lane == 0) sh.warp_above[warp] = above;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      lo = min(lo, sh.warp_lo[w]);
-      hi = max(hi, sh.warp_hi[w]);
-      rest -= sh.warp_above[w];
-    }
-    ch = choose<u64>(sh, keys, m, rest, lo, hi, turn);
-    for (int g = warp; g < groups; g += kWarps) {
-      const int i = 32 * g + lane;
-      const u64 k = i < m ? keys[i] : 0;
-      const unsigned ins = __ballot_sync(0xffffffffu, i < m && surely(ch, k)), eqs = __ballot_sync(0xffffffffu, i < m && equals(ch, k));
-      if (lane == 0) marks[g] = make_uint2(ins, eqs);
+    for (int w = 0; w < kWarps; ++w) rest -= sh.warp_above[w];
+    auto exact = [&](int i) {
+      int pg = ptx::ld_plain(table + i);
+      if ((unsigned)pg >= (unsigned)a.pool.num_pages) pg = 0;  // (reported above)
+      return exact_key<D>(q, base + pg * page_stride, G);
+    };
+    const int near_count = sh.near_count;
+    if (near_count <= kNear) {
+      for (int e = warp; e < near_count; e += kWarps) {
+        const u64 k = exact(sh.near_page[e]);
+        if (lane == 0) sh.near_key[e] = k;
+      }
+      __syncthreads();
+      if (warp == 0 && lane < near_count) {
+        const int i = sh.near_page[lane];
+        const u64 k = sh.near_key[lane];
+        int better = 0;
+        for (int e = 0; e < near_count; ++e) better += sh.near_key[e] > k || (sh.near_key[e] == k && sh.near_page[e] < i);
+        if (better < rest) atomicOr(&marks[i / 32].x, 1u << (i % 32));
+      }
+      ch.eq = 0;
+    } else {
+      u64 lo = kAbove, hi = kBelow;
+      for (int g = warp; g < groups; g += kWarps) {
+        const int i = 32 * g + lane;
+        const float v = i < m ? value_of(key_at<uint32_t>(keys, i)) : 0.f;
+        const bool over = i < m && v > low + 2.f * err, near = i < m && !over && !(v < low - 2.f * err);
+        u64 mine = over ? kAbove : kBelow;
+        for (unsigned open = __ballot_sync(0xffffffffu, near); open != 0; open &= open - 1) {
+          const int at = __ffs(open) - 1;
+          const u64 k = exact(32 * g + at);
+          if (lane == at) mine = k;
+          lo = min(lo, k);
+          hi = max(hi, k);
+        }
+        if (i < m) keys[i] = mine;
+      }
+      if (lane == 0) {
+        sh.warp_lo[warp] = lo;
+        sh.warp_hi[warp] = hi;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        lo = min(lo, sh.warp_lo[w]);
+        hi = max(hi, sh.warp_hi[w]);
+      }
+      ch = choose<u64>(sh, keys, m, rest, lo, hi, turn);
+      for (int g = warp; g < groups; g += kWarps) {
+        const int i = 32 * g + lane;
+        const u64 k = i < m ? keys[i] : 0;
+        const unsigned ins = __ballot_sync(0xffffffffu, i < m && surely(ch, k)), eqs = __ballot_sync(0xffffffffu, i < m && equals(ch, k));
+        if (lane == 0) marks[g] = make_uint2(ins, eqs);
+      }
     }
     __syncthreads();
   }
