@@ -5,6 +5,7 @@
 // 15.6 and 7.2), which bounded every small call: the kernel behind a decode of one sequence takes 4.2 us.
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -43,14 +44,22 @@ int size(const at::Tensor& t, int dim) {
   return (int)t.size(dim);
 }
 
-// What the calls around attention add to that: types and sizes, which a strided row would otherwise hide.
+// What the calls around attention add to that: the device, types and sizes, which a strided row would otherwise hide.
+void on_current_device(const at::Tensor& t) {
+  if (t.get_device() != c10::cuda::current_device()) raise(PyExc_ValueError, "tensor on another device than the current one");
+}
 const at::Tensor& typed(PyObject* o, at::ScalarType type) {
   const at::Tensor& t = tensor(o);
+  on_current_device(t);
   if (t.scalar_type() != type) raise(PyExc_TypeError, type == at::kInt ? "expected an int32 tensor" : type == at::kFloat ? "expected a float32 tensor" : "expected a bfloat16 tensor");
   return t;
 }
 void expect(bool ok, const char* what) {
   if (!ok) raise(PyExc_ValueError, what);
+}
+int count(int64_t n) {
+  expect(n <= 0x7fffffff, "more entries than an int holds");
+  return (int)n;
 }
 int* ints(PyObject* o, int64_t n, const char* what) {  // (None: nullptr)
   if (o == Py_None) return nullptr;
@@ -69,6 +78,7 @@ const at::Tensor& rows(PyObject* o) {
   if (!THPVariable_Check(o)) raise(PyExc_TypeError, "expected a torch tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
   if (!t.is_cuda()) raise(PyExc_AssertionError, "expected a CUDA tensor");
+  on_current_device(t);
   if (t.scalar_type() != at::kBFloat16) raise(PyExc_TypeError, "expected a bfloat16 tensor");
   expect(t.dim() == 3 && (t.size(2) < 2 || t.stride(2) == 1) && (t.size(1) < 2 || t.stride(1) == t.size(2)), "rows must be [tokens][heads][head_dim], dense inside a token");
   return t;
@@ -272,9 +282,9 @@ PyObject* step_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int *ctxp = read<int>(ctx), *freshp = read<int>(fresh);
     int *btp = written<int>(bt), *slotp = written<int>(slots);
     void* st = stream(a[11]);
-    const int pages = (int)fresh.numel(), width = size(bt, 1);
+    const int pages = count(fresh.numel()), width = count(bt.size(1)), n_seq = count(batch), n_rows = count(total);
     return unlocked([&] {
-      return kv_step_tables(p, ctxp, news, (int)batch, freshp, pages, btp, width, (int)total, cu, pos, slotp, next, cursor, next_cursor, st);
+      return kv_step_tables(p, ctxp, news, n_seq, freshp, pages, btp, width, n_rows, cu, pos, slotp, next, cursor, next_cursor, st);
     });
   });
 }
@@ -295,7 +305,7 @@ PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (has_q) {
       const at::Tensor& o = rows(a[8]);
       expect(o.sizes() == lead.sizes(), "q_out must have the shape of q");
-      q = read(lead), out = written(o), qs = lead.stride(0), os = o.stride(0), heads = size(lead, 1);
+      q = read(lead), out = written(o), qs = lead.stride(0), os = o.stride(0), heads = count(lead.size(1));
     }
     if (has_kv) {
       const at::Tensor &kt = rows(a[2]), &vt = rows(a[3]);
@@ -306,14 +316,14 @@ PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     expect(dim == integer(a[11]), "rows must have the pool's head_dim");
     const int* slots = read_ints(a[4], total, "slots must have an entry for each token");
     expect(pos.dim() >= 1 && pos.dim() <= 2 && pos.size(-1) == total, "positions must be [tokens] or [axes][tokens]");
-    const int axes = pos.dim() == 2 ? size(pos, 0) : 1, rot = 2 * (int)freq.numel();
+    const int axes = pos.dim() == 2 ? count(pos.size(0)) : 1, rot = count(2 * freq.numel()), n_rows = count(total);
     const int* axis = read_ints(a[7], freq.numel(), "freq_axis must have an entry for each frequency");
     const int* posp = read<int>(pos);
     const float* freqp = read<float>(freq);
     const int neighbours = integer(a[9]);
     void* st = stream(a[12]);
     return unlocked([&] {
-      return kv_append_rotary(p, q, qs, k, ks, v, vs, heads, slots, posp, axes, freqp, axis, rot, neighbours, (int)total, out, os, st);
+      return kv_append_rotary(p, q, qs, k, ks, v, vs, heads, slots, posp, axes, freqp, axis, rot, neighbours, n_rows, out, os, st);
     });
   });
 }
@@ -325,7 +335,7 @@ PyObject* page_bounds(PyObject*, PyObject* const* a, Py_ssize_t n) {
     expect(bounds.nbytes() >= kv_page_bounds_bytes(p), "bounds must have kv_page_bounds_bytes() bytes");
     const int* sp = read<int>(slots);
     void *bp = written(bounds), *st = stream(a[3]);
-    const int total = (int)slots.numel();
+    const int total = count(slots.numel());
     return unlocked([&] { return kv_page_bounds(p, sp, total, bp, st); });
   });
 }
@@ -340,12 +350,12 @@ PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
     expect(bt.size(0) == batch && list.size(0) == batch && list.size(1) == integer(a[11]), "block_tables and pages must have a row for each sequence, pages for each of the pool's heads");
     const int* ctx = read_ints(a[4], batch, "ctx_lens must have an entry for each sequence");
     int* counts = ints(a[9], batch * list.size(1), "counts must be [batch][kv heads]");
-    const int max_ctx = integer(a[5]), first = integer(a[6]), last = integer(a[7]), hq = size(q, 1), width = size(bt, 1), want = size(list, 2);
+    const int max_ctx = integer(a[5]), first = integer(a[6]), last = integer(a[7]), hq = count(q.size(1)), width = count(bt.size(1)), want = count(list.size(2)), n_seq = count(batch);
     const void *qp = read(q), *bp = read(bounds);
     const int* btp = read<int>(bt);
     int* lp = written<int>(list);
     void* st = stream(a[10]);
-    return unlocked([&] { return attn_select_pages(p, qp, hq, bp, btp, width, ctx, (int)batch, max_ctx, want, first, last, lp, counts, st); });
+    return unlocked([&] { return attn_select_pages(p, qp, hq, bp, btp, width, ctx, n_seq, max_ctx, want, first, last, lp, counts, st); });
   });
 }
 
@@ -359,13 +369,13 @@ PyObject* decode_selected(PyObject*, PyObject* const* a, Py_ssize_t n) {
     expect(out.sizes() == q.sizes() && lse.numel() == batch * q.size(1), "out must have the shape of q, lse an entry for each of its rows");
     const int* ctx = read_ints(a[3], batch, "ctx_lens must have an entry for each sequence");
     const int* counts = read_ints(a[6], batch * list.size(1), "counts must be [batch][kv heads]");
-    const int max_ctx = integer(a[4]), hq = size(q, 1), pages = size(bt, 1), width = size(list, 2);
+    const int max_ctx = integer(a[4]), hq = count(q.size(1)), pages = count(bt.size(1)), width = count(list.size(2)), n_seq = count(batch);
     const float scale = real(a[7]);
     const void* qp = read(q);
     const int *btp = read<int>(bt), *lp = read<int>(list);
     void *op = written(out), *st = stream(a[10]);
     float* lsep = written<float>(lse);
-    return unlocked([&] { return attn_decode_selected(p, qp, hq, btp, pages, ctx, (int)batch, max_ctx, lp, counts, width, scale, op, lsep, st); });
+    return unlocked([&] { return attn_decode_selected(p, qp, hq, btp, pages, ctx, n_seq, max_ctx, lp, counts, width, scale, op, lsep, st); });
   });
 }
 
