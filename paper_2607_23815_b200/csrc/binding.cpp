@@ -45,8 +45,10 @@ int size(const at::Tensor& t, int dim) {
 }
 
 // What the calls around attention add to that: the device, types and sizes, which a strided row would otherwise hide.
+thread_local int here = -1;  // the current device, once a call has asked
 void on_current_device(const at::Tensor& t) {
-  if (t.get_device() != c10::cuda::current_device()) raise(PyExc_ValueError, "tensor on another device than the current one");
+  if (here < 0) here = c10::cuda::current_device();
+  if (t.get_device() != here) raise(PyExc_ValueError, "tensor on another device than the current one");
 }
 const at::Tensor& typed(PyObject* o, at::ScalarType type) {
   const at::Tensor& t = tensor(o);
@@ -268,6 +270,7 @@ PyObject* mixed(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 PyObject* step_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  here = -1;
   return call(n, 12, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &ctx = typed(a[1], at::kInt), &fresh = typed(a[3], at::kInt), &bt = typed(a[4], at::kInt), &slots = typed(a[7], at::kInt);
@@ -290,6 +293,7 @@ PyObject* step_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  here = -1;
   return call(n, 13, [&] {
     kv_pool_t* p = pool(a[0]);
     const bool has_q = a[1] != Py_None, has_kv = a[2] != Py_None;
@@ -329,6 +333,7 @@ PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 PyObject* page_bounds(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  here = -1;
   return call(n, 4, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &slots = typed(a[1], at::kInt), &bounds = typed(a[2], at::kBFloat16);
@@ -341,6 +346,7 @@ PyObject* page_bounds(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  here = -1;
   return call(n, 12, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = typed(a[1], at::kBFloat16), &bounds = typed(a[2], at::kBFloat16), &bt = typed(a[3], at::kInt), &list = typed(a[8], at::kInt);
@@ -360,6 +366,7 @@ PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 PyObject* decode_selected(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  here = -1;
   return call(n, 12, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = typed(a[1], at::kBFloat16), &bt = typed(a[2], at::kInt), &list = typed(a[5], at::kInt), &out = typed(a[8], at::kBFloat16), &lse = typed(a[9], at::kFloat);
