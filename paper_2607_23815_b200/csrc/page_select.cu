@@ -183,8 +183,9 @@ __device__ __forceinline__ u64 exact_key(const __nv_bfloat16* q, const __nv_bflo
   return key_of(best);
 }
 
-template <int D, int kWarps>
-__global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(const SelectArgs a) {
+// kBlocks: blocks on an SM.  Of more than sixteen warps none has registers for a whole tile on its way.
+template <int D, int kWarps, int kBlocks>
+__global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(const SelectArgs a) {
   constexpr int NJ = D / 32;  // 16-byte chunks of lo (and of hi) of a page that a lane takes
   constexpr int kThreads = kWarps * 32;
   extern __shared__ u64 keys[];
@@ -253,58 +254,63 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
     const uint32_t keys0 = ptx::smem_u32(keys), keys_at = splits > 1 ? cluster_addr(keys0, 0) : keys0;
     uint32_t reach = 0, least = 0xffffffffu, most = 0;  // reach: the largest sum of the magnitudes of a score's terms (bits)
     const int tiles = (m + 15) / 16;
-    // A tile's two pages of this lane.  A part of a tile that has been multiplied is followed by the same part of the next tile, so that loads are under way
-    // all the time.
-    const uint4* src[2];
-    bool in[2];
+    // A tile's two pages of this lane.  A part of a tile that has been multiplied is followed by a part of the same or of the next tile, so that loads are
+    // under way all the time.
+    constexpr int kAhead = kWarps * kBlocks > 16 ? 1 : NJ;  // parts of a tile (of this, then of the next) that are on their way
+    struct Place { const uint4* src[2]; bool in[2]; };
     auto find = [&](int n, int tile) {  // the n-th tile of the warp, each once and in order
       if ((n & 1) == 0 && n > 0) {
         ids = ids_behind;
         ids_behind = table_entry(tile + 2 * runs, m);
       }
+      Place at;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         int pg = __shfl_sync(0xffffffffu, ids, 16 * (n & 1) + 8 * s + r);
-        in[s] = 16 * tile + 8 * s + r < m;
-        if (in[s] && (unsigned)pg >= (unsigned)a.pool.num_pages) {
+        at.in[s] = 16 * tile + 8 * s + r < m;
+        if (at.in[s] && (unsigned)pg >= (unsigned)a.pool.num_pages) {
           report(a.pool.status, KV_ERR_BOUNDS);
           pg = 0;  // stay inside; the result of this row is flagged, not trusted
         }
-        src[s] = reinterpret_cast<const uint4*>(base + pg * page_stride) + c;
+        at.src[s] = reinterpret_cast<const uint4*>(base + pg * page_stride) + c;
       }
+      return at;
     };
-    uint4 lo[NJ][2], hi[NJ][2];
-    auto load = [&](int j) {
+    uint4 lo[kAhead][2], hi[kAhead][2];
+    auto load = [&](const Place& at, int j) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        lo[j][s] = in[s] ? ldg_stream(src[s] + 4 * j) : make_uint4(0, 0, 0, 0);
-        hi[j][s] = in[s] ? ldg_stream(src[s] + D / 8 + 4 * j) : make_uint4(0, 0, 0, 0);
+        lo[j % kAhead][s] = at.in[s] ? ldg_stream(at.src[s] + 4 * j) : make_uint4(0, 0, 0, 0);
+        hi[j % kAhead][s] = at.in[s] ? ldg_stream(at.src[s] + D / 8 + 4 * j) : make_uint4(0, 0, 0, 0);
       }
     };
+    Place now{};
     if (run < tiles) {
-      find(0, run);
+      now = find(0, run);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) load(j);
+      for (int j = 0; j < kAhead; ++j) load(now, j);
     }
     __syncthreads();  // (the query is in shared memory)
     for (int tile = run, n = 0; tile < tiles; tile += runs, ++n) {
       const bool more = tile + runs < tiles;
-      if (more) find(n + 1, tile + runs);
+      Place then = now;
+      if (more) then = find(n + 1, tile + runs);
       // Sixteen terms to an accumulator of their own, these then added in a tree; the magnitudes of the terms, or more, in a chain beside them.
       float sum[NJ][4], mag[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const uint4 neg = sh.q[0][j][lane], pos = sh.q[1][j][lane], any = sh.q[2][j][lane];
         float part[4][4];
-        mma_bf16_16816_first(part[0], lo[j][0].x, lo[j][1].x, lo[j][0].y, lo[j][1].y, neg.x, neg.y);
-        mma_bf16_16816_first(part[1], lo[j][0].z, lo[j][1].z, lo[j][0].w, lo[j][1].w, neg.z, neg.w);
-        mma_bf16_16816_first(part[2], hi[j][0].x, hi[j][1].x, hi[j][0].y, hi[j][1].y, pos.x, pos.y);
-        mma_bf16_16816_first(part[3], hi[j][0].z, hi[j][1].z, hi[j][0].w, hi[j][1].w, pos.z, pos.w);
-        mma_bf16_16816(mag, larger(lo[j][0].x, hi[j][0].x), larger(lo[j][1].x, hi[j][1].x), larger(lo[j][0].y, hi[j][0].y), larger(lo[j][1].y, hi[j][1].y),
+        mma_bf16_16816_first(part[0], lo[j % kAhead][0].x, lo[j % kAhead][1].x, lo[j % kAhead][0].y, lo[j % kAhead][1].y, neg.x, neg.y);
+        mma_bf16_16816_first(part[1], lo[j % kAhead][0].z, lo[j % kAhead][1].z, lo[j % kAhead][0].w, lo[j % kAhead][1].w, neg.z, neg.w);
+        mma_bf16_16816_first(part[2], hi[j % kAhead][0].x, hi[j % kAhead][1].x, hi[j % kAhead][0].y, hi[j % kAhead][1].y, pos.x, pos.y);
+        mma_bf16_16816_first(part[3], hi[j % kAhead][0].z, hi[j % kAhead][1].z, hi[j % kAhead][0].w, hi[j % kAhead][1].w, pos.z, pos.w);
+        mma_bf16_16816(mag, larger(lo[j % kAhead][0].x, hi[j % kAhead][0].x), larger(lo[j % kAhead][1].x, hi[j % kAhead][1].x), larger(lo[j % kAhead][0].y, hi[j % kAhead][0].y), larger(lo[j % kAhead][1].y, hi[j % kAhead][1].y),
                        any.x, any.y);
-        mma_bf16_16816(mag, larger(lo[j][0].z, hi[j][0].z), larger(lo[j][1].z, hi[j][1].z), larger(lo[j][0].w, hi[j][0].w), larger(lo[j][1].w, hi[j][1].w),
+        mma_bf16_16816(mag, larger(lo[j % kAhead][0].z, hi[j % kAhead][0].z), larger(lo[j % kAhead][1].z, hi[j % kAhead][1].z), larger(lo[j % kAhead][0].w, hi[j % kAhead][0].w), larger(lo[j % kAhead][1].w, hi[j % kAhead][1].w),
                        any.z, any.w);
-        if (more) load(j);
+        if (j + kAhead < NJ) load(now, j + kAhead);
+        else if (more) load(then, j + kAhead - NJ);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[j][e] = (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
       }
@@ -314,6 +320,7 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
         for (int j = 0; j + step < NJ; j += 2 * step)
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[j][e] += sum[j + step][e];
+      now = then;
       // elements 0, 1: page r, heads 2c and 2c + 1; 2, 3: page r + 8
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -513,10 +520,10 @@ __global__ void __launch_bounds__(kWarps * 32, 16 / kWarps) select_pages_kernel(
 // Shared memory for the keys of so many pages and for the marks.
 static int select_smem(int pages) { return pages * 8 + (pages + 31) / 32 * 8; }
 
-template <int D, int kWarps>
+template <int D, int kWarps, int kBlocks>
 static kv_status_t launch_select(const kv_pool_t* p, const SelectArgs& a, int rows, cudaStream_t st) {
   static std::atomic<bool> ready[kMaxDevices];
-  if (!allow_smem((const void*)select_pages_kernel<D, kWarps>, select_smem(kSelMaxPages), ready, p->device)) return KV_ERR_CUDA;
+  if (!allow_smem((const void*)select_pages_kernel<D, kWarps, kBlocks>, select_smem(kSelMaxPages), ready, p->device)) return KV_ERR_CUDA;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
   cfg.gridDim = dim3((unsigned)(rows * a.splits));
@@ -530,7 +537,7 @@ static kv_status_t launch_select(const kv_pool_t* p, const SelectArgs& a, int ro
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = a.splits > 1 ? 2 : 1;
-  KV_CUDA_OK(cudaLaunchKernelEx(&cfg, select_pages_kernel<D, kWarps>, a));
+  KV_CUDA_OK(cudaLaunchKernelEx(&cfg, select_pages_kernel<D, kWarps, kBlocks>, a));
   count_launch();
   return KV_OK;
 }
@@ -574,9 +581,17 @@ extern "C" kv_status_t attn_select_pages(kv_pool_t* p, const void* q, int n_q_he
       a.splits = s;
     }
   if (a.splits == kSelMaxSplits && rows * 16 * a.splits <= resident && tiles > 4 * a.splits * warps) warps = 16;
-  const auto go = [&](auto w) {
-    return p->head_dim == 128 ? launch_select<128, decltype(w)::value>(p, a, (int)rows, (cudaStream_t)stream)
-                              : launch_select<64, decltype(w)::value>(p, a, (int)rows, (cudaStream_t)stream);
+  // Many rows of few pages take longer to begin and to choose than to read: seven blocks to an SM then, without whole tiles on their way.  Us with four /
+  // seven: heads of 128, 800 rows of 32-44 pages 10.2 / 9.9, 2048 of 19-38 19.3 / 15.4; of 64, 1000 of 42 10.8 / 8.5, 1600 of 63-188 21.3 / 19.6; longer
+  // rows, 1280 of 125-375, 38.7 / 46.5; fewer rows, heads of 64, 480 of 125-375, 11.7 / 13.5.
+  const bool brief = warps == 4 && rows > 4 * sms && tiles <= 12;
+  const auto go = [&](auto w, auto b) {
+    return p->head_dim == 128 ? launch_select<128, decltype(w)::value, decltype(b)::value>(p, a, (int)rows, (cudaStream_t)stream)
+                              : launch_select<64, decltype(w)::value, decltype(b)::value>(p, a, (int)rows, (cudaStream_t)stream);
   };
-  return warps == 16 ? go(std::integral_constant<int, 16>()) : warps == 8 ? go(std::integral_constant<int, 8>()) : go(std::integral_constant<int, 4>());
+  using std::integral_constant;
+  return warps == 16  ? go(integral_constant<int, 16>(), integral_constant<int, 1>())
+         : warps == 8 ? go(integral_constant<int, 8>(), integral_constant<int, 2>())
+         : brief      ? go(integral_constant<int, 4>(), integral_constant<int, 7>())
+                      : go(integral_constant<int, 4>(), integral_constant<int, 4>());
 }

@@ -149,3 +149,11 @@ def test_refusals():
             kvattn.attn_select_pages(pages.pool, *[bad if j == i else x for j, x in enumerate(ok)])
     kvattn.attn_select_pages(pages.pool, *ok)
     assert ok[7].flatten().tolist() == [0, 1, 0, 1] and pages.status() == 0
+
+
+@pytest.mark.parametrize("hq,hkv,d,n,ctx", [(32, 8, 128, 90, (300, 900)), (8, 8, 64, 100, (17, 3000)), (64, 8, 128, 80, (2900, 3200))])
+def test_more_rows_than_the_device_holds(hq, hkv, d, n, ctx):
+    rng = np.random.default_rng(n)
+    lens = rng.integers(ctx[0], ctx[1] + 1, n).tolist()
+    q, bounds, tables, count = _case(rng, hq, hkv, d, lens)
+    _check(q, bounds, tables, lens, hkv, count, 7, 1, 1)
