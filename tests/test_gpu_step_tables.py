@@ -48,7 +48,7 @@ def _compare(got, want, positions=True):
 
 SHAPES = [  # sequences, tokens before, new tokens, rows of padding
     (1, (0, 0), (1, 1), 0), (1, (16, 16), (1, 1), 3), (1, (15, 15), (1, 1), 0), (1, (1483, 1483), (37, 37), 0), (3, (0, 50), (0, 40), 5),
-    (251, (1024, 4095), (1, 1), 5), (511, (0, 40), (0, 3), 0), (512, (0, 40), (0, 3), 1), (513, (0, 40), (0, 3), 2), (1600, (0, 33), (0, 40), 7),
+    (251, (1024, 4095), (1, 1), 5), (255, (0, 40), (0, 3), 0), (256, (0, 40), (0, 3), 1), (257, (0, 40), (0, 3), 2), (511, (0, 40), (0, 3), 0), (512, (0, 40), (0, 3), 1), (513, (0, 40), (0, 3), 2), (1600, (0, 33), (0, 40), 7),
     (40, (0, 200), (300, 9000), 64), (7, (5, 5), (0, 0), 0), (7, (5, 5), (0, 0), 9), (1, (3, 3), (200001, 200001), 0)]
 
 
