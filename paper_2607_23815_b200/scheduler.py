@@ -559,13 +559,22 @@ class LibraryExecutor:
     attn_extend_append of its extend tokens over the pages it reuses, every generated token is a kv_append of that
     token's K/V and an attn_decode over the task's context.  Q/K/V are seeded synthetic values keyed on (task,
     position); nothing here checks numerics (the parity tests do), it checks that the scheduler's page bookkeeping is
-    what the kernels can run on: every call must leave the device status clean."""
+    what the kernels can run on: every call must leave the device status clean.
 
-    def __init__(self, pool, geom, seed: int = 0, device="cuda"):
+    decode_pages: a generated token attends over that many pages of its context only (the first, the newest and those that
+    attn_select_pages picks for it by their bounds, which are kept up with every append); None: over all of them."""
+
+    def __init__(self, pool, geom, seed: int = 0, device="cuda", decode_pages: Optional[int] = None):
         import torch
         from . import kvattn, synth
         self.torch, self.kv, self.synth = torch, kvattn, synth
         self.pool, self.geom, self.seed, self.device = pool, geom, seed, device
+        if decode_pages is not None and decode_pages < 2:
+            raise ValueError("decode_pages: the first page, the newest, and more")
+        self.decode_pages = decode_pages
+        self.bounds = None
+        if decode_pages is not None:
+            self.bounds = torch.empty(kvattn.kv_page_bounds_bytes(pool) // 2, dtype=torch.bfloat16, device=device)
         self.calls = {"extend_append": 0, "append": 0, "decode": 0}
         self.rows = {"prefill": 0, "decode": 0}
 
@@ -578,6 +587,12 @@ class LibraryExecutor:
     def _tables(self, tasks):
         width = max(len(t.table) for t in tasks)
         return self._i32([t.table + [-1] * (width - len(t.table)) for t in tasks])
+
+    def _renew_bounds(self, ranges):
+        """ranges: (task, first position, one past the last) of the tokens that have just been stored."""
+        if self.bounds is not None:
+            slots = [t.table[p // PAGE] * PAGE + p % PAGE for t, lo, hi in ranges for p in range(lo, hi)]
+            self.kv.kv_page_bounds(self.pool, self._i32(slots), self.bounds)
 
     def prefill(self, tasks):
         g, sy, torch = self.geom, self.synth, self.torch
@@ -596,6 +611,7 @@ class LibraryExecutor:
                          dtype=torch.uint8, device=self.device)
         self.kv.attn_extend_append(self.pool, q, k, v, cu, self._tables(tasks), self._i32(P), self._i32(E), max(E), max_l,
                                    g.scale, out, lse, ws)
+        self._renew_bounds([(t, t.reuse_tokens, t.reuse_tokens + t.extend_tokens) for t in tasks])
         self.calls["extend_append"] += 1
         self.rows["prefill"] += int(q.shape[0])
         self.last_out = out
@@ -611,9 +627,18 @@ class LibraryExecutor:
         ctx = [p + 1 for p in pos]
         out = torch.empty_like(q)
         lse = torch.empty((len(tasks), g.n_q_heads), dtype=torch.float32, device=self.device)
-        ws = torch.empty(max(256, self.kv.attn_workspace_bytes(self.pool, g.n_q_heads, 0, 0, 0, len(tasks), max(ctx))),
-                         dtype=torch.uint8, device=self.device)
-        self.kv.attn_decode(self.pool, q, bt, self._i32(ctx), max(ctx), g.scale, out, lse, ws)
+        if self.bounds is None:
+            ws = torch.empty(max(256, self.kv.attn_workspace_bytes(self.pool, g.n_q_heads, 0, 0, 0, len(tasks), max(ctx))),
+                             dtype=torch.uint8, device=self.device)
+            self.kv.attn_decode(self.pool, q, bt, self._i32(ctx), max(ctx), g.scale, out, lse, ws)
+        else:
+            self._renew_bounds([(t, p, p + 1) for t, p in zip(tasks, pos)])
+            lens = self._i32(ctx)
+            pages = torch.empty((len(tasks), g.n_kv_heads, min(self.decode_pages, pages_for(max(ctx)) + 1)), dtype=torch.int32, device=self.device)
+            counts = torch.empty((len(tasks), g.n_kv_heads), dtype=torch.int32, device=self.device)
+            self.kv.attn_select_pages(self.pool, q, self.bounds, bt, lens, max(ctx), 1, 1, pages, counts)
+            self.kv.attn_decode_selected(self.pool, q, bt, lens, max(ctx), pages, counts, g.scale, out, lse)
+            self.last_counts = counts
         self.calls["append"] += 1
         self.calls["decode"] += 1
         self.rows["decode"] += len(tasks)
