@@ -352,7 +352,8 @@ kv_status_t kv_page_bounds(kv_pool_t* pool, const int* slots, int total_new, voi
  * [n_kv_heads] how many.  ctx_lens[i] <= 0: none.  max_ctx_len: host upper bound; a longer sequence is recorded as KV_ERR_BOUNDS and its
  * rows are left unwritten, and so is a block-table entry outside the pool (its row's pages are then not to be trusted).
  * Table entries past the context may be read and are not used.
- * KV_ERR_INVALID: n_first + n_last > n_select.  KV_ERR_UNSUPPORTED: max_ctx_len above 24576 pages. */
+ * KV_ERR_INVALID: n_first + n_last > n_select.  KV_ERR_UNSUPPORTED: max_ctx_len above 24576 pages, or more than 64 GB of
+ * bounds. */
 kv_status_t attn_select_pages(kv_pool_t* pool, const void* q, int n_q_heads, const void* bounds, const int* block_tables, int max_pages,
                               const int* ctx_lens, int batch, int max_ctx_len, int n_select, int n_first, int n_last, int* pages,
                               int* counts, void* stream);

@@ -11,8 +11,8 @@
 // What bounds it: HBM (4 D bytes a page and KV head, read once) where there are many rows, latency where there are few, so a row's pages are then
 // shared out over a cluster whose CTAs push their scores into the shared memory of the first, which chooses.  A score is a product of (q+, q-), the
 // positive and the negative part of q, with (hi, lo): sixteen pages by eight heads in an mma.sync.m16n8k16 whose A fragments are the 16-byte chunks as
-// they lie.  (The lanes' own multiplications, G for every element, and their sums by shuffles took 103 us where this takes 26; the tensor
-// pipe is busy a tenth of the time.)  32 documents of 8192-16384 tokens, 64/8 heads of 128: 26.2 us, 3.8 TB/s; 15 us of it are the bytes, the rest is what a
+// they lie.  (The lanes' own multiplications, G for every element, and their sums by shuffles took 103 us where this takes 25; the tensor
+// pipe is busy a tenth of the time.)  32 documents of 8192-16384 tokens, 64/8 heads of 128: 25.4 us, 3.9 TB/s; 15 us of it are the bytes, the rest is what a
 // row has in front of them (length, page ids, the first pages: three trips to memory) and behind them (the choice, 2 to 3 us), at which no other row's
 // pages are read: the rows are on the device all at once.  256 sequences of 1024-4096: 42 us, 4.1 TB/s.  One of 15000: 5.7 us.  What has been left:
 // rows of the next round fetched in front of the choice, which only batches of more than four rows to an SM would gain by.
@@ -44,6 +44,7 @@ constexpr int kSelMaxWarps = 16;
 constexpr int kSelMaxPages = 24576;  // 198 KB of keys and marks
 constexpr int kBins = 256;
 constexpr int kNear = 32;
+constexpr int kFew = 128;  // pages whose order is found by comparing each with each
 typedef unsigned long long u64;
 
 // Keys in the order of the values, whatever is not a number above all of them; -0 and 0 are the same.  A page has room for 64 bits in shared memory:
@@ -188,13 +189,17 @@ template <int D, int kWarps, int kBlocks>
 __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(const SelectArgs a) {
   constexpr int NJ = D / 32;  // 16-byte chunks of lo (and of hi) of a page that a lane takes
   constexpr int kThreads = kWarps * 32;
+  constexpr bool kRanks = kBlocks == 7;  // (a kernel for rows of few pages)
   extern __shared__ u64 keys[];
   __shared__ __align__(16) SelectShared sh;
+  __shared__ __align__(16) uint32_t few_keys[kRanks ? kFew : 4];  // 0 behind the last
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int splits = a.splits, row = blockIdx.x / splits, rank = blockIdx.x - row * splits;
   const int Hkv = a.pool.n_kv_heads, G = a.group, seq = row / Hkv, kvh = row - seq * Hkv;
   const int runs = kWarps * splits, run = rank * kWarps + warp;
   for (int b = tid; b < kBins; b += kThreads) sh.hist[0][b] = 0;
+  if constexpr (kRanks)
+    for (int i = tid; i < kFew; i += kThreads) few_keys[i] = 0;
   if (tid == 0) sh.near_count = 0;
   if (splits > 1) cluster_arrive();
   ptx::dependency_wait();
@@ -246,18 +251,21 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
   const int m = nb - a.n_first - a.n_last, need = a.n_select - a.n_first - a.n_last;  // key i is that of page n_first + i
   const int64_t page_stride = (int64_t)Hkv * 2 * D;
   const __nv_bfloat16* base = a.bounds + (int64_t)kvh * 2 * D;
-  const bool all = nb <= a.n_select, scored = !all && need > 0;
+  const bool all = nb <= a.n_select, scored = !all && need > 0, few = kRanks && m <= kFew;
 
   // ---- scores
   if (scored) {
     if (splits > 1) cluster_wait();  // the first CTA runs: its shared memory may be written
-    const uint32_t keys0 = ptx::smem_u32(keys), keys_at = splits > 1 ? cluster_addr(keys0, 0) : keys0;
+    // where the keys are in this CTA and in the first
+    const uint32_t keys_here = few ? ptx::smem_u32(few_keys) : ptx::smem_u32(keys) + 4, keys_at = splits > 1 ? cluster_addr(keys_here, 0) : keys_here;
+    const uint32_t key_step = few ? 4 : 8;
     uint32_t reach = 0, least = 0xffffffffu, most = 0;  // reach: the largest sum of the magnitudes of a score's terms (bits)
     const int tiles = (m + 15) / 16;
     // A tile's two pages of this lane.  A part of a tile that has been multiplied is followed by a part of the same or of the next tile, so that loads are
     // under way all the time.
+    const uint4* all_bounds = reinterpret_cast<const uint4*>(a.bounds);
     constexpr int kAhead = kWarps * kBlocks > 16 ? 1 : NJ;  // parts of a tile (of this, then of the next) that are on their way
-    struct Place { const uint4* src[2]; bool in[2]; };
+    struct Place { uint32_t src[2]; bool in[2]; };  // (in 16 bytes: 32 bits reach further than any pool's bounds)
     auto find = [&](int n, int tile) {  // the n-th tile of the warp, each once and in order
       if ((n & 1) == 0 && n > 0) {
         ids = ids_behind;
@@ -272,7 +280,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
           report(a.pool.status, KV_ERR_BOUNDS);
           pg = 0;  // stay inside; the result of this row is flagged, not trusted
         }
-        at.src[s] = reinterpret_cast<const uint4*>(base + pg * page_stride) + c;
+        at.src[s] = ((uint32_t)pg * Hkv + kvh) * (D / 4) + c;
       }
       return at;
     };
@@ -280,8 +288,8 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
     auto load = [&](const Place& at, int j) {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        lo[j % kAhead][s] = at.in[s] ? ldg_stream(at.src[s] + 4 * j) : make_uint4(0, 0, 0, 0);
-        hi[j % kAhead][s] = at.in[s] ? ldg_stream(at.src[s] + D / 8 + 4 * j) : make_uint4(0, 0, 0, 0);
+        lo[j % kAhead][s] = at.in[s] ? ldg_stream(all_bounds + at.src[s] + 4 * j) : make_uint4(0, 0, 0, 0);
+        hi[j % kAhead][s] = at.in[s] ? ldg_stream(all_bounds + at.src[s] + D / 8 + 4 * j) : make_uint4(0, 0, 0, 0);
       }
     };
     Place now{};
@@ -332,7 +340,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
           const uint32_t key = key_of(best);
           least = min(least, key);
           most = max(most, key);
-          if (c == s) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys_at + i * 8 + 4), "r"(key) : "memory");
+          if (c == s) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(keys_at + i * key_step), "r"(key) : "memory");
         }
         reach = max(reach, max(__float_as_uint(mag[2 * s]) & 0x7fffffffu, __float_as_uint(mag[2 * s + 1]) & 0x7fffffffu));  // (not a number: above all)
       }
@@ -342,7 +350,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
     most = __reduce_max_sync(0xffffffffu, most);
     if (lane == 0) {
       const uint32_t lo0 = ptx::smem_u32(&sh.run_lo[run]), hi0 = ptx::smem_u32(&sh.run_hi[run]), reach0 = ptx::smem_u32(&sh.run_reach[run]);
-      const uint32_t shift = keys_at - keys0;  // to the first CTA
+      const uint32_t shift = keys_at - keys_here;  // to the first CTA
       asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(lo0 + shift), "r"(least) : "memory");
       asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(hi0 + shift), "r"(most) : "memory");
       asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(reach0 + shift), "r"(reach) : "memory");
@@ -369,17 +377,72 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
   if (!scored) return;
 
   // ---- the choice, by the first CTA
-  uint32_t least = 0xffffffffu, most = 0, reach = 0;
-  for (int i = lane; i < runs; i += 32) {
-    least = min(least, sh.run_lo[i]);
-    most = max(most, sh.run_hi[i]);
-    reach = max(reach, sh.run_reach[i]);
-  }
-  least = __reduce_min_sync(0xffffffffu, least);
-  most = __reduce_max_sync(0xffffffffu, most);
-  reach = __reduce_max_sync(0xffffffffu, reach);
+  // marks: of each 32 keys, those surely chosen and those that are equal to the last one chosen
+  const int groups = (m + 31) / 32;
+  uint2* marks = reinterpret_cast<uint2*>(keys + a.bound_pages);
+  auto approximate = [&](int i) { return few ? few_keys[i] : key_at<uint32_t>(keys, i); };
+  Choice ch{0, 0};
+  uint32_t kept, left;  // the smallest key chosen, the largest one left
   int turn = 0;
-  Choice ch = choose<uint32_t>(sh, keys, m, need, least, most, turn);
+  if (few) {
+    // Every key's rank: how many are larger, or equal and in front of it.  1000 rows of 42 pages 8.5 -> 7.6 us, 800 of 32-44, heads of 128, 9.9 -> 8.3; with
+    // 188 pages it is slower than counting by bits.
+    for (int g = warp; g < groups; g += kWarps) {
+      const int i = 32 * g + lane;
+      const uint32_t k = few_keys[i];
+      int rank = 0;
+      auto count = [&](int from, int to, auto limit) {
+#pragma unroll 8
+        for (int q = from / 4; q < to / 4; ++q) {
+          const uint4 x = reinterpret_cast<const uint4*>(few_keys)[q];
+          rank += (x.x > limit(4 * q)) + (x.y > limit(4 * q + 1)) + (x.z > limit(4 * q + 2)) + (x.w > limit(4 * q + 3));
+        }
+      };
+      count(0, 32 * g, [&](int) { return k - 1; });
+      count(32 * g, 32 * g + 32, [&](int j) { return j < i ? k - 1 : k; });
+      count(32 * g + 32, 32 * groups, [&](int) { return k; });
+      const bool in = i < m && rank < need;
+      const unsigned ins = __ballot_sync(0xffffffffu, in);
+      if (lane == 0) marks[g] = make_uint2(ins, 0);
+      if (i < m && rank == need - 1) sh.warp_kept[0] = k;
+      if (i < m && rank == need) sh.warp_left[0] = k;
+    }
+    __syncthreads();
+    kept = sh.warp_kept[0];
+    left = sh.warp_left[0];
+  } else {
+    uint32_t least = 0xffffffffu, most = 0;
+    for (int i = lane; i < runs; i += 32) {
+      least = min(least, sh.run_lo[i]);
+      most = max(most, sh.run_hi[i]);
+    }
+    least = __reduce_min_sync(0xffffffffu, least);
+    most = __reduce_max_sync(0xffffffffu, most);
+    ch = choose<uint32_t>(sh, keys, m, need, least, most, turn);
+    kept = 0xffffffffu;
+    left = 0;
+    for (int g = warp; g < groups; g += kWarps) {
+      const int i = 32 * g + lane;
+      const uint32_t k = i < m ? key_at<uint32_t>(keys, i) : 0;
+      const bool in = i < m && surely(ch, k), eq = i < m && equals(ch, k);
+      const unsigned ins = __ballot_sync(0xffffffffu, in), eqs = __ballot_sync(0xffffffffu, eq);
+      if (in || eq) kept = min(kept, k);
+      if (i < m && !in) left = max(left, k);  // (of equals, some are chosen and some are left)
+      if (lane == 0) marks[g] = make_uint2(ins, eqs);
+    }
+    kept = __reduce_min_sync(0xffffffffu, kept);
+    left = __reduce_max_sync(0xffffffffu, left);
+    if (lane == 0) {
+      sh.warp_kept[warp] = kept;
+      sh.warp_left[warp] = left;
+    }
+    __syncthreads();
+    kept = __reduce_min_sync(0xffffffffu, lane < kWarps ? sh.warp_kept[lane] : 0xffffffffu);
+    left = __reduce_max_sync(0xffffffffu, lane < kWarps ? sh.warp_left[lane] : 0);
+  }
+  uint32_t reach = 0;
+  for (int i = lane; i < runs; i += 32) reach = max(reach, sh.run_reach[i]);
+  reach = __reduce_max_sync(0xffffffffu, reach);
   // Of what the terms' magnitudes add up to, an accumulator loses 2^-23 with each of its sixteen terms at most, the tree 2^-24 with each of its four
   // steps: below 2^-18.8 in all; their sum as computed, by an accumulator of 128 terms, is short by 2^-16 of itself at most.  Elements of the bounds below
   // the normal numbers may count as 0 (2^-126 |q_d| each), as may sums.
@@ -387,28 +450,6 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
 #pragma unroll
   for (int j = 0; j < NJ; ++j) qsum += sh.qsum[j];
   const float err = __uint_as_float(reach) * 0x1p-18f + qsum * 0x1p-125f + 0x1p-120f;
-  // marks: of each 32 keys, those surely chosen and those that are equal to the last one chosen
-  const int groups = (m + 31) / 32;
-  uint2* marks = reinterpret_cast<uint2*>(keys + a.bound_pages);
-  uint32_t kept = 0xffffffffu, left = 0;  // the smallest key chosen, the largest one left
-  for (int g = warp; g < groups; g += kWarps) {
-    const int i = 32 * g + lane;
-    const uint32_t k = i < m ? key_at<uint32_t>(keys, i) : 0;
-    const bool in = i < m && surely(ch, k), eq = i < m && equals(ch, k);
-    const unsigned ins = __ballot_sync(0xffffffffu, in), eqs = __ballot_sync(0xffffffffu, eq);
-    if (in || eq) kept = min(kept, k);
-    if (i < m && !in) left = max(left, k);  // (of equals, some are chosen and some are left)
-    if (lane == 0) marks[g] = make_uint2(ins, eqs);
-  }
-  kept = __reduce_min_sync(0xffffffffu, kept);
-  left = __reduce_max_sync(0xffffffffu, left);
-  if (lane == 0) {
-    sh.warp_kept[warp] = kept;
-    sh.warp_left[warp] = left;
-  }
-  __syncthreads();
-  kept = __reduce_min_sync(0xffffffffu, lane < kWarps ? sh.warp_kept[lane] : 0xffffffffu);
-  left = __reduce_max_sync(0xffffffffu, lane < kWarps ? sh.warp_left[lane] : 0);
   const float low = value_of(kept), next = value_of(left);
   if (!(low - next > 2.f * err)) {
     // Those above the band around the border are chosen, those in it scored again: a few, to each warp its share, of which every lane then sees whether
@@ -416,7 +457,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
     int above = 0, rest = need;
     for (int g = warp; g < groups; g += kWarps) {
       const int i = 32 * g + lane;
-      const float v = i < m ? value_of(key_at<uint32_t>(keys, i)) : 0.f;
+      const float v = i < m ? value_of(approximate(i)) : 0.f;
       const bool over = i < m && v > low + 2.f * err, near = i < m && !over && !(v < low - 2.f * err);
       const unsigned overs = __ballot_sync(0xffffffffu, over);
       above += __popc(overs);
@@ -454,7 +495,7 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
       u64 lo = kAbove, hi = kBelow;
       for (int g = warp; g < groups; g += kWarps) {
         const int i = 32 * g + lane;
-        const float v = i < m ? value_of(key_at<uint32_t>(keys, i)) : 0.f;
+        const float v = i < m ? value_of(approximate(i)) : 0.f;
         const bool over = i < m && v > low + 2.f * err, near = i < m && !over && !(v < low - 2.f * err);
         u64 mine = over ? kAbove : kBelow;
         for (unsigned open = __ballot_sync(0xffffffffu, near); open != 0; open &= open - 1) {
@@ -561,6 +602,7 @@ extern "C" kv_status_t attn_select_pages(kv_pool_t* p, const void* q, int n_q_he
   if (!on_pool_device(p)) return KV_ERR_INVALID;
   const int64_t rows = (int64_t)batch * p->n_kv_heads, bound = ((int64_t)max_ctx_len + kPageSize - 1) / kPageSize;
   if (bound > kSelMaxPages || rows * kSelMaxSplits > 0x7fffffffLL) return KV_ERR_UNSUPPORTED;
+  if ((int64_t)p->num_pages * p->n_kv_heads * (p->head_dim / 4) > 0xffffffffLL) return KV_ERR_UNSUPPORTED;  // (64 GB of bounds)
   SelectArgs a{p->view(), (const __nv_bfloat16*)q, (const __nv_bfloat16*)bounds, block_tables, ctx_lens, pages, counts, max_pages, (int)bound,
                group, n_select, n_first, n_last, 1};
   // CTAs of eight warps, two of them to an SM, or of four, four to an SM, and as many to a row as the device holds and find sixteen pages for most of
@@ -582,8 +624,8 @@ extern "C" kv_status_t attn_select_pages(kv_pool_t* p, const void* q, int n_q_he
     }
   if (a.splits == kSelMaxSplits && rows * 16 * a.splits <= resident && tiles > 4 * a.splits * warps) warps = 16;
   // Many rows of few pages take longer to begin and to choose than to read: seven blocks to an SM then, without whole tiles on their way.  Us with four /
-  // seven: heads of 128, 800 rows of 32-44 pages 10.2 / 9.9, 2048 of 19-38 19.3 / 15.4; of 64, 1000 of 42 10.8 / 8.5, 1600 of 63-188 21.3 / 19.6; longer
-  // rows, 1280 of 125-375, 38.7 / 46.5; fewer rows, heads of 64, 480 of 125-375, 11.7 / 13.5.
+  // seven (before the ranks): heads of 128, 800 rows of 32-44 pages 10.2 / 9.9, 2048 of 19-38 19.3 / 15.4; of 64, 1000 of 42 10.8 / 8.5, 1600 of 63-188
+  // 21.3 / 19.6; longer rows, 1280 of 125-375, 38.7 / 46.5; fewer rows, heads of 64, 480 of 125-375, 11.7 / 13.5.
   const bool brief = warps == 4 && rows > 4 * sms && tiles <= 12;
   const auto go = [&](auto w, auto b) {
     return p->head_dim == 128 ? launch_select<128, decltype(w)::value, decltype(b)::value>(p, a, (int)rows, (cudaStream_t)stream)

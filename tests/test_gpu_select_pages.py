@@ -157,3 +157,22 @@ def test_more_rows_than_the_device_holds(hq, hkv, d, n, ctx):
     lens = rng.integers(ctx[0], ctx[1] + 1, n).tolist()
     q, bounds, tables, count = _case(rng, hq, hkv, d, lens)
     _check(q, bounds, tables, lens, hkv, count, 7, 1, 1)
+
+
+@pytest.mark.parametrize("what", ["normal", "equal", "few_values", "not_numbers"])
+def test_many_rows_of_few_pages(what):
+    rng = np.random.default_rng(6)
+    hq, hkv, d = 16, 8, 64
+    lens = rng.integers(1, 190 * 16, 90).tolist()
+    lens[:12] = [16 * n for n in (8, 9, 39, 40, 41, 71, 72, 73, 134, 135, 136, 137)]   # (up to 128 pages in question, and more)
+    q, bounds, tables, count = _case(rng, hq, hkv, d, lens)
+    if what == "equal":
+        bounds[:] = bounds[:1]
+    if what == "few_values":
+        bounds = np.sign(bounds) * (rng.integers(0, 3, (count, 1, 1, 1)) + 1.0)
+        bounds = np.stack([bounds.min(2), bounds.max(2)], 2)
+    if what == "not_numbers":
+        bounds[rng.integers(0, count, count // 9), :, 1, 3] = np.nan
+        bounds[rng.integers(0, count, count // 9), :, 0, 4] = -np.inf
+    for n_select, first, last in ((8, 1, 2), (40, 0, 0), (5, 3, 2)):
+        _check(q, orc.widen(_bits(bounds)), tables, lens, hkv, count, n_select, first, last)
