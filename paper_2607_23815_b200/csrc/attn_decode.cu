@@ -71,7 +71,8 @@ constexpr int decode_smem_bytes() {
   return (RING ? DecodeSmem<D>::kRing : DecodeSmem<D>::kPart) + DecodeSmem<D>::kIn + (int)sizeof(DecodeShared);
 }
 
-// SEL: the pages of a pair are those of its list, not all of the sequence's.
+// SEL: the pages of a pair are those of its list, not all of the sequence's (one more load in front of the table's; the rules below take a list for a
+// context of its length).  256 lists of 64 pages, 32/8 heads of 128: 158 us, 6.8 TB/s; 32 of 128, 64/8 heads, 45.3 (41.2 at the copy rate); one of 64 4.9.
 // MULTI: several pairs per CTA (a.per_cta > 1).  An instantiation of its own: with the pair as a run-time value everywhere the
 // others lost 0.3 us (13 sequences of 200-3000 tokens, 64 dims, 13.2 -> 13.5; one of 517 4.25 -> 4.5).
 template <int D, bool RING, bool MULTI, bool SEL>
