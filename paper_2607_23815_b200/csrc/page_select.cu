@@ -364,7 +364,6 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
   } else if (splits > 1) {
     cluster_wait();
   }
-  ptx::launch_dependents();
   if (rank != 0 || !fits) return;
   if (all) {
     for (int i = tid; i < a.n_select; i += kThreads) list[i] = i < nb ? i : -1;
@@ -528,6 +527,10 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocks) select_pages_kernel(cons
     __syncthreads();
   }
 
+  // The kernel behind this one is let in when the choice is made.  Decode's blocks, let in when the scores were there, took what room these left on the
+  // SMs and their clusters found no places beside each other: steps of 9, 30 and 64 sequences (tables, rotary append, bounds, choice, decode; 1000-2000 tokens)
+  // 25.5 / 31.4 / 44.9 us, this way 21.3 / 31.2 / 44.5, on two streams 12.9 / 24.2 / 37.8 and 12.8 / 21.8 / 34.7; of one 16.7 and 16.9.
+  ptx::launch_dependents();
   // ---- the list, ascending: every warp counts all the marks, 32 groups at a time, and writes the groups that are its own
   int out = a.n_first, eq_before = 0;
   for (int g0 = 0; g0 < groups; g0 += 32) {
@@ -610,12 +613,14 @@ extern "C" kv_status_t attn_select_pages(kv_pool_t* p, const void* q, int n_q_he
   // 1 / 2 / 4 (heads of 128, 8 to a group): 8 rows of 722 pages 12.0 / 9.1 / 7.9 / 6.7, 16.1 / 11.1 / 8.3; 64 rows of 512-1024 19.8 / 16.8 / 14.6 / 17.8,
   // 27.0 / 19.9 / 16.2; 240 of 63-94 7.7 / 12.6 / - / -, 8.0 / 8.1 / 11.7; 256 of 512-1024 28.4 / 33.1 / - / -, 35.5 / 29.4 / 30.8; 2048 of 64-256 56.0
   // and 41.7 with one.  Few rows that are longer still: sixteen warps, 8 rows of 6250 pages, heads of 64, 15.6 / 13.1 with eight / sixteen.
+  // An eighth of the device stays free beside clusters: those that do not find their CTAs' places at once, because of the kernel in front or of how they
+  // fall on the SMs, are a second round (96 rows of 188-375 pages 10.9 us with three CTAs each, 9.3 with two; 192 of 63-125 8.8 and 7.3).
   const int sms = sm_count_of(p->device);
   const int64_t tiles = (bound + 15) / 16, resident = 16 * (int64_t)sms;  // (warps)
   int warps = 4;
   double least = 1e30;
   for (int w : {8, 4})
-    for (int s = 1; s <= kSelMaxSplits && (s == 1 || (rows * s * w <= resident && 2 * tiles > (int64_t)s * w)); ++s) {
+    for (int s = 1; s <= kSelMaxSplits && (s == 1 || (8 * rows * s * w <= 7 * resident && 2 * tiles > (int64_t)s * w)); ++s) {
       const double most = (double)((rows * s + sms - 1) / sms) / s;
       if ((w == 8 && rows * w > resident) || most > (w == 8 ? least : 0.9 * least)) continue;
       least = most;
