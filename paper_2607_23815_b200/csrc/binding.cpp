@@ -347,10 +347,11 @@ PyObject* page_bounds(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
   here = -1;
-  return call(n, 12, [&] {
+  return call(n, 13, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = typed(a[1], at::kBFloat16), &bounds = typed(a[2], at::kBFloat16), &bt = typed(a[3], at::kInt), &list = typed(a[8], at::kInt);
     expect(q.dim() == 3 && bt.dim() == 2 && list.dim() == 3, "q must be [batch][heads][head_dim], block_tables [batch][pages], pages [batch][kv heads][n]");
+    expect(q.size(2) == integer(a[12]), "q must have the pool's head_dim");
     const int64_t batch = q.size(0);
     expect(bounds.nbytes() >= kv_page_bounds_bytes(p), "bounds must have kv_page_bounds_bytes() bytes");
     expect(bt.size(0) == batch && list.size(0) == batch && list.size(1) == integer(a[11]), "block_tables and pages must have a row for each sequence, pages for each of the pool's heads");
@@ -367,10 +368,11 @@ PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* decode_selected(PyObject*, PyObject* const* a, Py_ssize_t n) {
   here = -1;
-  return call(n, 12, [&] {
+  return call(n, 13, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = typed(a[1], at::kBFloat16), &bt = typed(a[2], at::kInt), &list = typed(a[5], at::kInt), &out = typed(a[8], at::kBFloat16), &lse = typed(a[9], at::kFloat);
     expect(q.dim() == 3 && bt.dim() == 2 && list.dim() == 3, "q must be [batch][heads][head_dim], block_tables [batch][pages], pages [batch][kv heads][n]");
+    expect(q.size(2) == integer(a[12]), "q must have the pool's head_dim");
     const int64_t batch = q.size(0);
     expect(bt.size(0) == batch && list.size(0) == batch && list.size(1) == integer(a[11]), "block_tables and pages must have a row for each sequence, pages for each of the pool's heads");
     expect(out.sizes() == q.sizes() && lse.numel() == batch * q.size(1), "out must have the shape of q, lse an entry for each of its rows");

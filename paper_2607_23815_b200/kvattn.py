@@ -395,13 +395,13 @@ def kv_page_bounds(pool: Pool, slots, bounds, stream=None):
 def attn_select_pages(pool: Pool, q, bounds, block_tables, ctx_lens, max_ctx_len, n_first, n_last, pages, counts, stream=None):
     """Writes, for every sequence and KV head, the pages.shape[2] pages that its query can have the largest scores with."""
     _check(_native.attn_select_pages(pool.ptr, q, bounds, block_tables, ctx_lens, max_ctx_len, n_first, n_last, pages, counts, stream,
-                                     pool.n_kv_heads), "attn_select_pages")
+                                     pool.n_kv_heads, pool.head_dim), "attn_select_pages")
 
 
 def attn_decode_selected(pool: Pool, q, block_tables, ctx_lens, max_ctx_len, pages, counts, scale, out, lse, stream=None):
     """attn_decode over the listed pages of each sequence and KV head."""
     _check(_native.attn_decode_selected(pool.ptr, q, block_tables, ctx_lens, max_ctx_len, pages, counts, scale, out, lse, stream,
-                                        pool.n_kv_heads), "attn_decode_selected")
+                                        pool.n_kv_heads, pool.head_dim), "attn_decode_selected")
 
 
 def kv_check_batch(pool: Pool, block_tables, lens, stream=None) -> int:
