@@ -89,6 +89,7 @@ const at::Tensor& rows(PyObject* o) {
 int integer(PyObject* o) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) throw Raised{};
+  if (v != (int)v) raise(PyExc_OverflowError, "whole number beyond an int");  // (its lower half would pass for another number)
   return (int)v;
 }
 float real(PyObject* o) {
