@@ -11,11 +11,10 @@
 #include <vector>
 
 #include "../../include/kvattn.h"
+#include "lengths.h"
 #include "spread.h"
 
 namespace kvattn {
-
-constexpr int kPageSize = 16;
 
 // Device-visible description of the pool, passed to kernels by value.
 struct PoolView {

@@ -81,8 +81,7 @@ __global__ void __launch_bounds__(kTableThreads) step_tables_kernel(const Tables
     unsigned all_rows, all_pages;
     const unsigned row = add_limited(rows, block_sum(n_rows, warp_sums, &all_rows)), row_end = add_limited(row, n_rows);
     bool ok = c >= 0 && n >= 0 && (int64_t)c + n <= room && row_end <= (unsigned)a.total_new;
-    const int have = ok ? (int)(((int64_t)c + kPageSize - 1) / kPageSize) : 0;
-    const unsigned need = ok ? (unsigned)(((int64_t)c + n + kPageSize - 1) / kPageSize) - have : 0;
+    const unsigned need = ok ? pages_of(c + n) - pages_of(c) : 0;
     const unsigned page = add_limited(pages, block_sum(need, warp_sums, &all_pages)), page_end = add_limited(page, need);
     if (need > 0 && page_end > avail) ok = false;  // the list has run out: this sequence and the later ones that need a page get none
     first_row[tid] = in ? row : kSumLimit;
@@ -110,7 +109,7 @@ __global__ void __launch_bounds__(kTableThreads) step_tables_kernel(const Tables
         int pos = 0, slot = -1;
         if (ctx[lo] >= 0) {
           pos = ctx[lo] + (int)(t - first_row[lo]);
-          const int b = pos / kPageSize, owned = (ctx[lo] + kPageSize - 1) / kPageSize;
+          const int b = pos / kPageSize, owned = pages_of(ctx[lo]);
           int* entry = a.block_tables + (int64_t)(base + lo) * a.max_pages + b;
           const bool fresh = b >= owned;
           const int page = ptx::ld_plain(fresh ? a.new_pages + cursor + first_page[lo] + (b - owned) : entry);
