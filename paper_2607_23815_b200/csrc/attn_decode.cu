@@ -109,10 +109,10 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
 
   const int L = ptx::ld_plain(a.ctx_lens + seq);
   const int in_list = SEL ? ptx::ld_plain(a.lists.counts + unit) : 0;
-  const bool fits = L <= a.max_pages * kPageSize && L <= a.len_bound && (!SEL || (unsigned)in_list <= (unsigned)a.lists.width);
+  const bool fits = L <= a.max_pages * (int64_t)kPageSize && L <= a.len_bound && (!SEL || (unsigned)in_list <= (unsigned)a.lists.width);
   if (!fits && rank == 0 && lane == 0) report(a.pool.status, KV_ERR_BOUNDS);  // left unwritten
   if (MULTI && lane == 0 && warp == mine * team) sh.fits[mine] = fits;
-  const int blocks = fits && L > 0 && !idle ? (L + kPageSize - 1) / kPageSize : 0;  // of the sequence
+  const int blocks = fits && L > 0 && !idle ? pages_of(L) : 0;  // of the sequence
   const int n_pages = !SEL ? blocks : blocks > 0 ? in_list : 0;
   const int runs = team * splits;
   const int run = rank * team + warp - mine * team;
@@ -137,8 +137,8 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
     const size_t page_stride = (size_t)Hkv * blk;
     const int* bt_row = a.block_tables + (int64_t)seq * a.max_pages;
     const int* list = SEL ? a.lists.pages + (int64_t)unit * a.lists.width : nullptr;
-    // p: place in the pair's run of pages; block: which of the sequence's it is (SEL: as listed; none, all of whose keys are
-    // hidden, if the sequence has no such block)
+    // p: place in the pair's run of pages; block: which of the sequence's it is (SEL: as listed; one past its last, all of
+    // whose keys are hidden, if the sequence has no such block)
     auto table_entry = [&](int p, int& block) {
       int pg = 0;
       block = p;
@@ -175,7 +175,8 @@ __global__ void __launch_bounds__(kWarps * 32) attn_decode_kernel(const DecodeAr
         nxt = table_entry(base + 32 + lane, nxt_block);
       }
     };
-    auto first_token = [&](int p) { return (SEL ? __shfl_sync(0xffffffffu, cur_block, (p - base) & 31) : p) * kPageSize; };  // p in [base, base + 32)
+    // (without a sign: the block one past the last of the longest sequence begins at 2^31)
+    auto first_token = [&](int p) { return (unsigned)(SEL ? __shfl_sync(0xffffffffu, cur_block, (p - base) & 31) : p) * kPageSize; };  // p in [base, base + 32)
     if constexpr (RING) {
       const uint32_t slots = ptx::smem_u32(smem_raw) + warp * (kStages * SM::kSlot);
       const uint32_t bars = ptx::smem_u32(&sh.bars[warp * kStages]);
@@ -469,7 +470,7 @@ static kv_status_t pairs_per_cta(const kv_pool_t* p, int64_t units, int max_ctx_
 // sequences), 7.8 / 8.0 (3.1), with more CTAs than are resident 45.6 / 47.1 (6.0), 97.8 / 114.1 (6.0); 64 dims 4.6 / 4.2 (0.8), 5.4 /
 // 5.1 (1.6), 6.6 / 6.0 (2.75), 10.6 / 11.2 (4.2).
 static bool few_pages(const kv_pool_t* p, int64_t blocks, int warps, int max_ctx_len) {
-  const double pages = (double)(max_ctx_len + kPageSize - 1) / kPageSize / warps;
+  const double pages = ((double)max_ctx_len + kPageSize - 1) / kPageSize / warps;
   return pages <= (p->head_dim == 64 ? 2.75 : blocks <= 2 * sm_count_of(p->device) ? 2.0 : 1.0);
 }
 

@@ -143,10 +143,10 @@ struct RowState {
 
 // Takes the page of tokens tok0 .. tok0 + 15 into the running softmax.  qf: fragments of the query rows (row r's 16-byte
 // chunks 4j + c); limit0 / limit1: keys the rows n0 / n1 see; L: tokens of the sequence (slots at or past it hold
-// arbitrary bits).
+// arbitrary bits).  Places are numbers without a sign: the end of the last page of 2^31 - 1 tokens is 2^31.
 template <int D>
-__device__ __forceinline__ void page_step(RowState<D>& st, PageRegs<D>& pr, const uint4 (&qf)[D / 32], int tok0, int limit0,
-                                          int limit1, int L, float scale_log2, int r, int c) {
+__device__ __forceinline__ void page_step(RowState<D>& st, PageRegs<D>& pr, const uint4 (&qf)[D / 32], unsigned tok0, unsigned limit0,
+                                          unsigned limit1, unsigned L, float scale_log2, int r, int c) {
   constexpr int NJ = D / 32, NU = D / 64;
   // ---- S^T[16 tokens][8 rows] = K Q^T, in two accumulators: the chain of dependent MMAs is what a page's latency starts with
   float s[4] = {0.f, 0.f, 0.f, 0.f}, t[4] = {0.f, 0.f, 0.f, 0.f};
@@ -156,7 +156,7 @@ __device__ __forceinline__ void page_step(RowState<D>& st, PageRegs<D>& pr, cons
     mma_bf16_16816(t, pr.k[0][j].z, pr.k[1][j].z, pr.k[0][j].w, pr.k[1][j].w, qf[j].z, qf[j].w);
   }
   // s00: (token r, row n0)  s01: (token r, n1)  s10: (token r+8, n0)  s11: (token r+8, n1)
-  const int ta = tok0 + r, tb = tok0 + r + 8;
+  const unsigned ta = tok0 + r, tb = tok0 + r + 8;
   const float s00 = ta < limit0 ? (s[0] + t[0]) * scale_log2 : -INFINITY;
   const float s01 = ta < limit1 ? (s[1] + t[1]) * scale_log2 : -INFINITY;
   const float s10 = tb < limit0 ? (s[2] + t[2]) * scale_log2 : -INFINITY;
