@@ -297,8 +297,9 @@ kv_status_t attn_mixed(kv_pool_t* pool, int n_q_heads, float scale, const attn_e
  * (The paper has no counterpart of these calls: its engine does this work.  They take a step from its sequences' lengths and the
  * projected rows of its tokens to stored pages, and a query to the pages worth attending over.)
  * A slot is a place for a token: 16 * page + place in the page.  A slot map has a slot for every row of a step, or a negative
- * number for a row of padding; the rows that go into one page follow one another in increasing slots, each slot once, as they
- * do when every sequence's rows are in order.  Pools of more than 2^27 pages: KV_ERR_UNSUPPORTED. */
+ * number for a row of padding; the rows that go into one page follow one another, no other row between them, in increasing slots,
+ * each slot once, as they do when every sequence's rows are in order.  Slots that are left out between two of them stay as they are.
+ * Pools of more than 2^27 pages: KV_ERR_UNSUPPORTED. */
 
 /* Block tables, positions and slots of a step, from lengths that are on the device.  Sequence i holds ctx_lens[i] tokens and stores
  * new_lens[i] more (0 or more; ctx_lens, new_lens [dev][batch]).  Each page that this opens is taken from new_pages [dev]

@@ -105,7 +105,9 @@ __global__ void __launch_bounds__(kRotaryWarps * 32, kRotaryBlocks) append_rotar
       ptx::launch_dependents();
       let_in = true;
     }
-    const bool clears = follow != slot + 1;  // the last row of its page clears the slots behind it, as kv_append's does
+    // The last row of its page clears the slots behind it, as kv_append's does.  One that another row of the page follows does not, even if slots are
+    // left out between them: another warp may be storing that row.
+    const bool clears = (unsigned)follow / kPageSize != (unsigned)slot / kPageSize;
     if (slot < 0) continue;  // a padding row: nothing of it is written
     const int page = slot / kPageSize, at = slot % kPageSize;
     if (page >= a.pool.num_pages) {
