@@ -363,7 +363,8 @@ kv_status_t attn_select_pages(kv_pool_t* pool, const void* q, int n_q_heads, con
  * sequence i only (pages [dev][batch][n_kv_heads][width], counts [dev][batch][n_kv_heads], as attn_select_pages writes them; any order,
  * each block once).  counts 0 or ctx_lens[i] <= 0 writes O = 0, LSE = -inf.  Entries of the list past the count are not read.
  * A listed block that the sequence has not got is passed over, and a count outside 0 .. width leaves the rows of its KV head unwritten;
- * both are recorded as KV_ERR_BOUNDS.  No workspace.  Other arguments and errors as for attn_decode. */
+ * both are recorded as KV_ERR_BOUNDS.  No workspace.  The first call on a device prepares all variants of its kernel (attn_decode's first call
+ * does not).  Other arguments and errors as for attn_decode. */
 kv_status_t attn_decode_selected(kv_pool_t* pool, const void* q, int n_q_heads, const int* block_tables, int max_pages, const int* ctx_lens,
                                  int batch, int max_ctx_len, const int* pages, const int* counts, int width, float scale, void* out,
                                  float* lse, void* stream);

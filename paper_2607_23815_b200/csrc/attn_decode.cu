@@ -337,18 +337,17 @@ static kv_status_t prepare_variant() {
 }
 
 // Prepares the kernel for a device, once, and every variant at a time: which one a later call takes depends on its batch and
-// lengths, and callers that may not allocate (attn_decode_static) or that capture make one call of any shape beforehand.
+// lengths, and callers that may not allocate (attn_decode_static) or that capture make one call of any shape beforehand.  The variants
+// over lists (SEL) are prepared by the first call that has one: 0.3 ms and 2 MB of device memory that a user without lists does without.
+template <bool SEL>
 static kv_status_t decode_setup(int device) {
   static std::atomic<bool> configured[kMaxDevices];
   if (device < 0 || device >= kMaxDevices) return KV_ERR_INVALID;
   if (!configured[device].load(std::memory_order_acquire)) {
     kv_status_t (*const all[])() = {
-        prepare_variant<128, true, false, false>, prepare_variant<128, false, false, false>, prepare_variant<128, true, true, false>,
-        prepare_variant<128, false, true, false>, prepare_variant<64, true, false, false>,   prepare_variant<64, false, false, false>,
-        prepare_variant<64, true, true, false>,   prepare_variant<64, false, true, false>,   prepare_variant<128, true, false, true>,
-        prepare_variant<128, false, false, true>, prepare_variant<128, true, true, true>,    prepare_variant<128, false, true, true>,
-        prepare_variant<64, true, false, true>,   prepare_variant<64, false, false, true>,   prepare_variant<64, true, true, true>,
-        prepare_variant<64, false, true, true>};
+        prepare_variant<128, true, false, SEL>, prepare_variant<128, false, false, SEL>, prepare_variant<128, true, true, SEL>,
+        prepare_variant<128, false, true, SEL>, prepare_variant<64, true, false, SEL>,   prepare_variant<64, false, false, SEL>,
+        prepare_variant<64, true, true, SEL>,   prepare_variant<64, false, true, SEL>};
     for (const auto prepare : all) {
       const kv_status_t s = prepare();
       if (s != KV_OK) return s;
@@ -381,7 +380,7 @@ static constexpr int kSplitChoices[] = {1, 2, 3, 4, 6, 8, 16};
 template <int D>
 static kv_status_t resident_clusters(int device, int i, int* n) {
   static std::atomic<int> cached[kMaxDevices][sizeof(kSplitChoices) / sizeof(int)];  // value + 1
-  const kv_status_t s = decode_setup(device);
+  const kv_status_t s = decode_setup<false>(device);
   if (s != KV_OK) return s;
   int v = cached[device][i].load(std::memory_order_relaxed);
   if (v == 0) {
@@ -476,7 +475,7 @@ static bool few_pages(const kv_pool_t* p, int64_t blocks, int warps, int max_ctx
 
 template <int D, bool RING, bool MULTI, bool SEL>
 static kv_status_t launch_decode_variant(const kv_pool_t* p, const DecodeArgs& a, int64_t blocks, cudaStream_t st) {
-  const kv_status_t s = decode_setup(p->device);
+  const kv_status_t s = decode_setup<SEL>(p->device);
   if (s != KV_OK) return s;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr[2];
