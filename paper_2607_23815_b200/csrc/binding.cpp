@@ -44,6 +44,24 @@ int size(const at::Tensor& t, int dim) {
   return (int)t.size(dim);
 }
 
+void expect(bool ok, const char* what) {
+  if (!ok) raise(PyExc_ValueError, what);
+}
+// The kernels go by the pool's head_dim: rows of another size would be read, and results written, past their ends.
+void of_pool(const kv_pool_t* p, const at::Tensor& t, const char* what) {
+  if (p != nullptr && t.dim() == 3) expect(t.size(2) == kv_pool_elem_offset(p, 0, 0, 8, 0) / 8, what);  // (slot 8 of a block lies eight rows behind its first)
+}
+void rows_of_pool(const kv_pool_t* p, const at::Tensor& q) { of_pool(p, q, "q must have the pool's head_dim"); }
+void new_rows_of_pool(const kv_pool_t* p, const at::Tensor& k, const at::Tensor& v) {
+  of_pool(p, k, "k_new must have the pool's head_dim");
+  expect(v.nbytes() >= k.nbytes(), "v_new must have the shape of k_new");
+}
+// (both may be larger: buffers for the largest step there is)
+void results_hold(const at::Tensor& q, const at::Tensor& out, const at::Tensor& lse) {
+  expect(out.nbytes() >= q.nbytes(), "out must have the shape of q");
+  expect(lse.numel() >= q.size(0) * q.size(1), "lse must have an entry for each row of q");
+}
+
 // What the calls around attention add to that: the device, types and sizes, which a strided row would otherwise hide.
 thread_local int here = -1;  // the current device, once a call has asked
 void on_current_device(const at::Tensor& t) {
@@ -55,9 +73,6 @@ const at::Tensor& typed(PyObject* o, at::ScalarType type) {
   on_current_device(t);
   if (t.scalar_type() != type) raise(PyExc_TypeError, type == at::kInt ? "expected an int32 tensor" : type == at::kFloat ? "expected a float32 tensor" : "expected a bfloat16 tensor");
   return t;
-}
-void expect(bool ok, const char* what) {
-  if (!ok) raise(PyExc_ValueError, what);
 }
 int count(int64_t n) {
   expect(n <= 0x7fffffff, "more entries than an int holds");
@@ -171,6 +186,7 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &k = tensor(a[1]), &start = tensor(a[4]), &bt = tensor(a[6]);
     const void *kp = read(k), *vp = read(a[2]);
+    if (a[2] != Py_None) new_rows_of_pool(p, k, tensor(a[2]));
     const int *cu = read<int>(a[3]), *startp = read<int>(start), *row = read<int>(a[5]), *btp = read<int>(bt);
     void* st = stream(a[7]);
     const int pages = size(bt, 1), segs = (int)start.numel(), total = size(k, 0);
@@ -183,11 +199,13 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = tensor(a[1]), &bt = tensor(a[2]);
     const void* qp = read(q);
+    rows_of_pool(p, q);
     const int *btp = read<int>(bt), *ctx = read<int>(a[3]);
     const int max_ctx = integer(a[4]), hq = size(q, 1), pages = size(bt, 1), batch = size(q, 0);
     const float scale = real(a[5]);
     void *out = written(a[6]), *st = stream(a[9]);
     float* lse = written<float>(a[7]);
+    if (a[6] != Py_None && a[7] != Py_None) results_hold(q, tensor(a[6]), tensor(a[7]));
     const Workspace ws(a[8]);
     return unlocked([&] { return attn_decode(p, qp, hq, btp, pages, ctx, batch, max_ctx, scale, out, lse, ws.p, ws.bytes, st); });
   });
@@ -202,11 +220,14 @@ PyObject* extend_like(PyObject* const* a, Py_ssize_t n, int lead, F f) {  // lea
     PyObject* const* b = a + lead;
     const at::Tensor &bt = tensor(b[1]), &pl = tensor(b[2]);
     const void* qp = read(q);
+    rows_of_pool(p, q);
+    if (lead == 4 && a[2] != Py_None && a[3] != Py_None) new_rows_of_pool(p, tensor(a[2]), tensor(a[3]));
     const int *cu = read<int>(b[0]), *btp = read<int>(bt), *plp = read<int>(pl), *el = read<int>(b[3]);
     const int batch = (int)pl.numel(), max_e = integer(b[4]), max_l = integer(b[5]), hq = size(q, 1), total = size(q, 0), pages = size(bt, 1);
     const float scale = real(b[6]);
     void *out = written(b[7]), *st = stream(b[10]);
     float* lse = written<float>(b[8]);
+    if (b[7] != Py_None && b[8] != Py_None) results_hold(q, tensor(b[7]), tensor(b[8]));
     const Workspace ws(b[9]);
     const void *k = lead == 4 ? read(a[2]) : nullptr, *v = lead == 4 ? read(a[3]) : nullptr;
     return unlocked([&] {
@@ -242,12 +263,14 @@ PyObject* extend_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = tensor(a[1]), &pt = tensor(a[4]), &pl = tensor(a[5]), &ct = tensor(a[6]), &cl = tensor(a[7]);
     const void* qp = read(q);
+    rows_of_pool(p, q);
     const int *cu = read<int>(a[2]), *cc = read<int>(a[3]), *ptp = read<int>(pt), *plp = read<int>(pl), *ctp = read<int>(ct), *clp = read<int>(cl);
     const int max_c = integer(a[8]), max_rows = integer(a[9]), max_p = integer(a[10]), parents = (int)pl.numel(), children = (int)cl.numel();
     const int hq = size(q, 1), total = size(q, 0), pages_p = size(pt, 1), pages_c = size(ct, 1);
     const float scale = real(a[11]);
     void *out = written(a[12]), *st = stream(a[15]);
     float* lse = written<float>(a[13]);
+    if (a[12] != Py_None && a[13] != Py_None) results_hold(q, tensor(a[12]), tensor(a[13]));
     const Workspace ws(a[14]);
     return unlocked([&] {
       return attn_extend_shared(p, qp, hq, cu, cc, ptp, pages_p, plp, ctp, pages_c, clp, parents, children, total, max_c, max_rows, max_p,
@@ -348,11 +371,11 @@ PyObject* page_bounds(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
   here = -1;
-  return call(n, 13, [&] {
+  return call(n, 12, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = typed(a[1], at::kBFloat16), &bounds = typed(a[2], at::kBFloat16), &bt = typed(a[3], at::kInt), &list = typed(a[8], at::kInt);
     expect(q.dim() == 3 && bt.dim() == 2 && list.dim() == 3, "q must be [batch][heads][head_dim], block_tables [batch][pages], pages [batch][kv heads][n]");
-    expect(q.size(2) == integer(a[12]), "q must have the pool's head_dim");
+    rows_of_pool(p, q);
     const int64_t batch = q.size(0);
     expect(bounds.nbytes() >= kv_page_bounds_bytes(p), "bounds must have kv_page_bounds_bytes() bytes");
     expect(bt.size(0) == batch && list.size(0) == batch && list.size(1) == integer(a[11]), "block_tables and pages must have a row for each sequence, pages for each of the pool's heads");
@@ -369,11 +392,11 @@ PyObject* select_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 PyObject* decode_selected(PyObject*, PyObject* const* a, Py_ssize_t n) {
   here = -1;
-  return call(n, 13, [&] {
+  return call(n, 12, [&] {
     kv_pool_t* p = pool(a[0]);
     const at::Tensor &q = typed(a[1], at::kBFloat16), &bt = typed(a[2], at::kInt), &list = typed(a[5], at::kInt), &out = typed(a[8], at::kBFloat16), &lse = typed(a[9], at::kFloat);
     expect(q.dim() == 3 && bt.dim() == 2 && list.dim() == 3, "q must be [batch][heads][head_dim], block_tables [batch][pages], pages [batch][kv heads][n]");
-    expect(q.size(2) == integer(a[12]), "q must have the pool's head_dim");
+    rows_of_pool(p, q);
     const int64_t batch = q.size(0);
     expect(bt.size(0) == batch && list.size(0) == batch && list.size(1) == integer(a[11]), "block_tables and pages must have a row for each sequence, pages for each of the pool's heads");
     expect(out.sizes() == q.sizes() && lse.numel() == batch * q.size(1), "out must have the shape of q, lse an entry for each of its rows");
@@ -403,6 +426,9 @@ PyObject* extend_host(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const void *qp = read(q), *kp = read(k), *vp = read(v);
     const int *cup = read<int>(cu), *btp = read<int>(bt), *plp = read<int>(pl), *elp = read<int>(el);
     const int max_e = integer(a[8]), max_l = integer(a[9]), hq = size(q, 1), total = size(q, 0), pages = size(bt, 1), batch = (int)pl.numel();
+    rows_of_pool(p, q);
+    new_rows_of_pool(p, k, v);
+    results_hold(q, out, lse);
     const float scale = real(a[10]);
     void* outp = written(out);
     float* lsep = written<float>(lse);

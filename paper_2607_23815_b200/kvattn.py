@@ -343,6 +343,8 @@ def attn_decode(pool: Pool, q, block_tables, ctx_lens, max_ctx_len, scale, out, 
 def attn_decode_static(pool: Pool, q, block_tables, ctx_lens, max_ctx_len, scale, out, lse, stream=None):
     """attn_decode for callers that cannot allocate: the same launch without a workspace argument (see the header for the
     limit on the batch)."""
+    if q.shape[-1] != pool.head_dim or out.nbytes < q.nbytes or lse.numel() < q.shape[0] * q.shape[1]:
+        raise ValueError("q must have the pool's head_dim, out the shape of q and lse an entry for each of its rows")
     _check(lib().attn_decode_static(pool.handle, _dev_ptr(q), q.shape[1], _dev_ptr(block_tables),
                                     block_tables.shape[1], _dev_ptr(ctx_lens), q.shape[0], max_ctx_len, float(scale),
                                     _dev_ptr(out), _dev_ptr(lse), _stream(stream)), "attn_decode_static")
@@ -395,13 +397,13 @@ def kv_page_bounds(pool: Pool, slots, bounds, stream=None):
 def attn_select_pages(pool: Pool, q, bounds, block_tables, ctx_lens, max_ctx_len, n_first, n_last, pages, counts, stream=None):
     """Writes, for every sequence and KV head, the pages.shape[2] pages that its query can have the largest scores with."""
     _check(_native.attn_select_pages(pool.ptr, q, bounds, block_tables, ctx_lens, max_ctx_len, n_first, n_last, pages, counts, stream,
-                                     pool.n_kv_heads, pool.head_dim), "attn_select_pages")
+                                     pool.n_kv_heads), "attn_select_pages")
 
 
 def attn_decode_selected(pool: Pool, q, block_tables, ctx_lens, max_ctx_len, pages, counts, scale, out, lse, stream=None):
     """attn_decode over the listed pages of each sequence and KV head."""
     _check(_native.attn_decode_selected(pool.ptr, q, block_tables, ctx_lens, max_ctx_len, pages, counts, scale, out, lse, stream,
-                                        pool.n_kv_heads, pool.head_dim), "attn_decode_selected")
+                                        pool.n_kv_heads), "attn_decode_selected")
 
 
 def kv_check_batch(pool: Pool, block_tables, lens, stream=None) -> int:
