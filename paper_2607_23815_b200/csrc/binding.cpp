@@ -54,6 +54,8 @@ void of_pool(const kv_pool_t* p, const at::Tensor& t, const char* what) {
 void rows_of_pool(const kv_pool_t* p, const at::Tensor& q) { of_pool(p, q, "q must have the pool's head_dim"); }
 void new_rows_of_pool(const kv_pool_t* p, const at::Tensor& k, const at::Tensor& v) {
   of_pool(p, k, "k_new must have the pool's head_dim");
+  // (a place of a head that the pool has not got is -1)
+  if (p != nullptr && k.dim() == 3) expect(kv_pool_elem_offset(p, 0, size(k, 1) - 1, 0, 0) >= 0 && kv_pool_elem_offset(p, 0, size(k, 1), 0, 0) < 0, "k_new must have the pool's heads");
   expect(v.nbytes() >= k.nbytes(), "v_new must have the shape of k_new");
 }
 // (both may be larger: buffers for the largest step there is)
@@ -221,7 +223,10 @@ PyObject* extend_like(PyObject* const* a, Py_ssize_t n, int lead, F f) {  // lea
     const at::Tensor &bt = tensor(b[1]), &pl = tensor(b[2]);
     const void* qp = read(q);
     rows_of_pool(p, q);
-    if (lead == 4 && a[2] != Py_None && a[3] != Py_None) new_rows_of_pool(p, tensor(a[2]), tensor(a[3]));
+    if (lead == 4 && a[2] != Py_None && a[3] != Py_None) {
+      new_rows_of_pool(p, tensor(a[2]), tensor(a[3]));
+      expect(size(tensor(a[2]), 0) >= size(q, 0), "k_new must have a row for each of q's tokens");
+    }
     const int *cu = read<int>(b[0]), *btp = read<int>(bt), *plp = read<int>(pl), *el = read<int>(b[3]);
     const int batch = (int)pl.numel(), max_e = integer(b[4]), max_l = integer(b[5]), hq = size(q, 1), total = size(q, 0), pages = size(bt, 1);
     const float scale = real(b[6]);
@@ -428,6 +433,7 @@ PyObject* extend_host(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int max_e = integer(a[8]), max_l = integer(a[9]), hq = size(q, 1), total = size(q, 0), pages = size(bt, 1), batch = (int)pl.numel();
     rows_of_pool(p, q);
     new_rows_of_pool(p, k, v);
+    expect(size(k, 0) >= total, "k_new must have a row for each of q's tokens");
     results_hold(q, out, lse);
     const float scale = real(a[10]);
     void* outp = written(out);
