@@ -327,7 +327,8 @@ kv_status_t kv_step_tables(kv_pool_t* pool, const int* ctx_lens, const int* new_
  * Row r goes to slots[r] [dev][total_new]; the last row of a page clears the slots behind it, as kv_append does.  A row with a
  * negative slot is padding: nothing of it is written, q_out neither.  q (with q_out) may be NULL; k_new and v_new may both be NULL,
  * and then slots too.  q_out may be q (with the same stride); no other overlap.
- * KV_ERR_UNSUPPORTED: rot_dim not a multiple of 16 in 16 .. head_dim.  KV_ERR_INVALID: a pointer to rows not 16-byte aligned, or, with
+ * KV_ERR_UNSUPPORTED: rot_dim not a multiple of 16 in 16 .. head_dim, more than 2^15 query heads, or 2^31 pieces (eight heads of 128 dims, sixteen of
+ * 64) of rows in all.  KV_ERR_INVALID: a pointer to rows not 16-byte aligned, or, with
  * more than one row, a stride below a token's elements or not a multiple of 8.  A slot outside the pool (its row is skipped) or an axis outside 0 .. n_axes - 1 (axis 0 is
  * taken) is recorded as KV_ERR_BOUNDS. */
 kv_status_t kv_append_rotary(kv_pool_t* pool, const void* q, int64_t q_stride, const void* k_new, int64_t k_stride, const void* v_new,
@@ -351,10 +352,10 @@ kv_status_t kv_page_bounds(kv_pool_t* pool, const int* slots, int total_new, voi
  * q [dev] bf16 [batch][n_q_heads][head_dim]; bounds as kv_page_bounds writes them, for all those pages; pages [dev][batch][n_kv_heads]
  * [n_select] receives the pages as blocks of the sequence (indices into its block-table row), ascending, then -1; counts [dev][batch]
  * [n_kv_heads] how many.  ctx_lens[i] <= 0: none.  max_ctx_len: host upper bound; a longer sequence is recorded as KV_ERR_BOUNDS and its
- * rows are left unwritten, and so is a block-table entry outside the pool (its row's pages are then not to be trusted).
- * Table entries past the context may be read and are not used.
- * KV_ERR_INVALID: n_first + n_last > n_select.  KV_ERR_UNSUPPORTED: max_ctx_len above 24576 pages, or more than 64 GB of
- * bounds. */
+ * rows are left unwritten, and so is a block-table entry outside the pool of a page that is scored (its row's pages are then not to be
+ * trusted; pages that are chosen without a score are not looked up).  Table entries past the context may be read and are not used.
+ * KV_ERR_INVALID: n_first + n_last > n_select.  KV_ERR_UNSUPPORTED: query heads not 1, 2, 4 or 8 to a KV head, max_ctx_len above 24576
+ * pages, or more than 64 GB of bounds. */
 kv_status_t attn_select_pages(kv_pool_t* pool, const void* q, int n_q_heads, const void* bounds, const int* block_tables, int max_pages,
                               const int* ctx_lens, int batch, int max_ctx_len, int n_select, int n_first, int n_last, int* pages,
                               int* counts, void* stream);
@@ -363,7 +364,8 @@ kv_status_t attn_select_pages(kv_pool_t* pool, const void* q, int n_q_heads, con
  * sequence i only (pages [dev][batch][n_kv_heads][width], counts [dev][batch][n_kv_heads], as attn_select_pages writes them; any order,
  * each block once).  counts 0 or ctx_lens[i] <= 0 writes O = 0, LSE = -inf.  Entries of the list past the count are not read.
  * A listed block that the sequence has not got is passed over, and a count outside 0 .. width leaves the rows of its KV head unwritten;
- * both are recorded as KV_ERR_BOUNDS.  No workspace.  The first call on a device prepares all variants of its kernel (attn_decode's first call
+ * both are recorded as KV_ERR_BOUNDS.  Sums are held in 32 bits; a weight is rounded to bf16 before it multiplies a value, as in attn_decode
+ * (the same bits over all pages): 2^-8 of sum p |v| at most beside the rounding of O.  No workspace.  The first call on a device prepares all variants of its kernel (attn_decode's first call
  * does not).  Other arguments and errors as for attn_decode. */
 kv_status_t attn_decode_selected(kv_pool_t* pool, const void* q, int n_q_heads, const int* block_tables, int max_pages, const int* ctx_lens,
                                  int batch, int max_ctx_len, const int* pages, const int* counts, int width, float scale, void* out,

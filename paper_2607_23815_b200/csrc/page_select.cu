@@ -615,6 +615,9 @@ extern "C" kv_status_t attn_select_pages(kv_pool_t* p, const void* q, int n_q_he
   // and 41.7 with one.  Few rows that are longer still: sixteen warps, 8 rows of 6250 pages, heads of 64, 15.6 / 13.1 with eight / sixteen.
   // An eighth of the device stays free beside clusters: those that do not find their CTAs' places at once, because of the kernel in front or of how they
   // fall on the SMs, are a second round (96 rows of 188-375 pages 10.9 us with three CTAs each, 9.3 with two; 192 of 63-125 8.8 and 7.3).
+  // The rules go by the bound, and a block has shared memory for the keys of as many pages: a bound of 2 or 4 times the longest sequence costs at most 4 %,
+  // one of 16 times up to a third, where blocks stop fitting beside each other (32 documents of 8192-16384, 64/8 heads, 26.5 / 27.1 / 27.2 / 33.2 us
+  // with 1 / 2 / 4 / 16 times, 256 sequences of 1024-4096 42.2 / 41.9 / 42.4 / 47.4, 1000 rows of 42 pages 8.5 / 8.2 / 8.2 / 11.5).
   const int sms = sm_count_of(p->device);
   const int64_t tiles = (bound + 15) / 16, resident = 16 * (int64_t)sms;  // (warps)
   int warps = 4;
